@@ -360,6 +360,93 @@ t3_status t3_ag_step(const t3_problem *p, int32_t step, const float *upstream_R,
 #define T3_TIMELINE_ITEMS 16
 t3_status t3_timeline(uint64_t *stamps, int64_t words);
 
+/*
+ * ---- Products in 8-bit integers (a layer served in 8 bits).
+ *
+ * t3_quant_rows makes rows of 8-bit integers, each with a scale of its own, of an activation's rows (a scale per token) or of a
+ * weight's stored N x K (a scale per output channel): with a the largest magnitude of the row,
+ *
+ *   scale = a / 127 (rounded to fp32),   q = the integer nearest to 127 x / a, ties to even
+ *
+ * (the quotient is not rounded before).  A row of zeros has q = 0 and scale 0; a row with an infinity or a NaN q = 0 and
+ * scale NaN, so that products of it are NaN.
+ *
+ *   x      [rows][ldx], t3_type: bf16 (ldx a multiple of 8) or fp32 (of 4), read
+ *   q      [rows][ldq], ldq a multiple of 8, out: columns [0, cols); 8-byte aligned
+ *   scale  [rows], out
+ * cols a multiple of 8 (T3_ERR_ALIGN); x 16-byte, scale 4-byte aligned.
+ */
+typedef enum { T3_TYPE_BF16 = 0, T3_TYPE_F32 = 1 } t3_type;
+t3_status t3_quant_rows(int32_t rows, int32_t cols, int32_t x_type, const void *x, int64_t ldx, int8_t *q, int64_t ldq,
+                        float *scale, void *stream);
+
+/*
+ * t3_gemm and t3_gemm_rs_fused on such operands.  With q_A, q_B the integers,
+ *
+ *   C[m][n] = scale_a[m] scale_b[n] sum_k q_A[m][k] q_B[n][k]
+ *
+ * the sum in 32-bit integers, exact; as a float, times scale_a and times scale_b it is rounded once each (in the fused call the
+ * last together with the addition of the incoming partial; in a launch with a balanced tail a tile's sum is the fp32 sum of two such
+ * halves).  The result is fp32, added to R, forwarded and tracked as in t3_gemm_rs_fused.
+ *
+ *   A        int8 [M][lda], B int8 [N][ldb]: K-contiguous (T3_A_MK, T3_B_NK; T3_ERR_UNSUPPORTED otherwise)
+ *   scale_a  fp32 [M], scale_b fp32 [N], device, 4-byte aligned
+ * p is as for the bf16 calls with lda, ldb and K in elements of a byte: multiples of 16 (T3_ERR_ALIGN), K at most 131056, so that no
+ * sum leaves 32 bits, A and B below 2^32 bytes each (T3_ERR_UNSUPPORTED).  Neither two writers nor split-K, and a tile range is of whole
+ * ring steps (T3_ERR_UNSUPPORTED).
+ */
+t3_status t3_gemm_i8(const t3_problem *p, const int8_t *A, const float *scale_a, const int8_t *B, const float *scale_b,
+                     float *C, void *stream);
+t3_status t3_gemm_rs_fused_i8(const t3_problem *p, const int8_t *A, const float *scale_a, const int8_t *B,
+                              const float *scale_b, float *R, void *fwd, uint32_t *track, void *stream);
+
+/*
+ * ---- Products by group (the layers of experts: each row of A goes to one of `groups` weights).
+ *
+ * Rows of A (and of C) are sorted by group; group e has rows offsets[e] .. offsets[e+1] - 1.  `offsets` is device memory, read by the
+ * kernels: the host never needs the groups' sizes.  A group may have no rows.  Rows before offsets[0] and from
+ * offsets[groups] on belong to no group: they are not read, and C's are left as they are.  Offsets that are out of order or outside of
+ * [0, rows] are read as the nearest ones that are not (no access leaves the arrays).
+ */
+#define T3_MAX_GROUPS 256
+#define T3_GROUPED_ACCUMULATE 1u       /* t3_gemm_grouped_wgrad adds to what dB holds */
+typedef struct {
+  int32_t rows, groups;   /* rows of A and C, of all groups and of none; groups, 1 .. T3_MAX_GROUPS (T3_ERR_UNSUPPORTED beyond)  */
+  int32_t N, K;           /* columns of C; columns of A                                                                          */
+  int32_t b_layout;       /* t3_b_layout of every group's B                                                                      */
+  uint32_t flags;         /* T3_GROUPED_*                                                                                        */
+  int64_t lda, ldb, ldc;  /* leading dimensions in elements: of A (>= K), of a group's B (>= K for NK, >= N for KN), of C (>= N) */
+  int64_t stride_b;       /* elements from one group's B to the next one's (0: all groups share one)                             */
+} t3_grouped;
+
+/*
+ * C[r] = A[r] . B_e for every row r of group e.
+ *
+ *   offsets  int32 [groups + 1], device
+ *   A        bf16 [rows][lda], B bf16 at B + e stride_b, by b_layout; lda, ldb, stride_b and K multiples of 8
+ *   C        fp32 [rows][ldc], N and ldc multiples of 4; out: the groups' rows
+ * T3_B_KN is the gradient to the rows of a layer whose weights are stored N x K (K and N trade places): N a multiple of 8.  A and a group's B below 2^31 elements each, C below 2^32 bytes.
+ */
+t3_status t3_gemm_grouped(const t3_grouped *g, const int32_t *offsets, const void *A, const void *B, float *C,
+                          void *stream);
+
+/* The same in 8 bits (t3_quant_rows): A int8 [rows][lda], B int8, T3_B_NK, K, lda, ldb and stride_b multiples of 16; scale_a fp32
+   [rows], scale_b fp32 [groups][N].  Sums, roundings and K's limit as in t3_gemm_i8. */
+t3_status t3_gemm_grouped_i8(const t3_grouped *g, const int32_t *offsets, const int8_t *A, const float *scale_a,
+                             const int8_t *B, const float *scale_b, float *C, void *stream);
+
+/*
+ * The gradient of the groups' weights: dB_e = the sum over group e's rows r of dC[r] (x) A[r], in the layout of B (NK:
+ * dB_e[n][k] = sum dC[r][n] A[r][k]).  A group without rows has a gradient of zeros.
+ *
+ *   A   bf16 [rows][lda], dC bf16 [rows][ldc]; lda, ldc, N and K multiples of 8
+ *   dB  fp32 at dB + e stride_b, leading dimension ldb, both multiples of 4, groups not overlapping; out, or with
+ *       T3_GROUPED_ACCUMULATE added to
+ * A and dC below 2^31 elements each, a group's dB below 2^32 bytes.
+ */
+t3_status t3_gemm_grouped_wgrad(const t3_grouped *g, const int32_t *offsets, const void *A, const void *dC, float *dB,
+                                void *stream);
+
 const char *t3_status_string(t3_status s);
 
 /* hipError_t of the last T3_ERR_HIP on the calling thread (0 if none). */

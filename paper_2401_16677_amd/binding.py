@@ -21,11 +21,15 @@ T3_FLAG_TWO_WRITERS = 4
 T3_FLAG_FWD_BF16 = 8
 T3_STATIC_MAX_TP = 64
 T3_TIMELINE_ITEMS = 16
+T3_TYPE_BF16, T3_TYPE_F32 = 0, 1
+T3_MAX_GROUPS = 256
+T3_GROUPED_ACCUMULATE = 1
 
 EXPORTS = ["t3_chunk_order", "t3_default_tile", "t3_tiles_per_chunk", "t3_tile_of",
            "t3_track_words", "t3_track_reset", "t3_gemm_rs_fused", "t3_gemm", "t3_rs_reduce",
            "t3_upstream_update", "t3_release_chunks", "t3_gemm_rs_fused_static", "t3_ag_step",
-           "t3_timeline", "t3_status_string", "t3_last_hip_error"]
+           "t3_quant_rows", "t3_gemm_i8", "t3_gemm_rs_fused_i8", "t3_gemm_grouped", "t3_gemm_grouped_i8",
+           "t3_gemm_grouped_wgrad", "t3_timeline", "t3_status_string", "t3_last_hip_error"]
 
 
 class T3Problem(ctypes.Structure):
@@ -39,6 +43,13 @@ class T3Problem(ctypes.Structure):
                 ("tile_begin", ctypes.c_int64), ("split_k", ctypes.c_int32),
                 ("upstream_agents", ctypes.c_int32), ("a_layout", ctypes.c_int32),
                 ("reserved", ctypes.c_int32)]
+
+
+class T3Grouped(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("groups", ctypes.c_int32), ("N", ctypes.c_int32),
+                ("K", ctypes.c_int32), ("b_layout", ctypes.c_int32), ("flags", ctypes.c_uint32),
+                ("lda", ctypes.c_int64), ("ldb", ctypes.c_int64), ("ldc", ctypes.c_int64),
+                ("stride_b", ctypes.c_int64)]
 
 
 class T3Error(RuntimeError):
@@ -79,13 +90,21 @@ def lib():
         L.t3_rs_reduce.argtypes = [pp, vp, vp, vp, vp, vp]
         L.t3_upstream_update.argtypes = [pp, vp, vp, vp, vp]
         L.t3_release_chunks.argtypes = [pp, vp, vp, vp, vp]
+        gp = ctypes.POINTER(T3Grouped)
+        L.t3_quant_rows.argtypes = [i32, i32, i32, vp, i64, vp, i64, vp, vp]
+        L.t3_gemm_i8.argtypes = [pp, vp, vp, vp, vp, vp, vp]
+        L.t3_gemm_rs_fused_i8.argtypes = [pp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.t3_gemm_grouped.argtypes = [gp, vp, vp, vp, vp, vp]
+        L.t3_gemm_grouped_i8.argtypes = [gp, vp, vp, vp, vp, vp, vp, vp]
+        L.t3_gemm_grouped_wgrad.argtypes = [gp, vp, vp, vp, vp, vp]
         L.t3_status_string.argtypes = [ctypes.c_int]
         L.t3_status_string.restype = ctypes.c_char_p
         L.t3_last_hip_error.restype = i32
         for f in ("t3_chunk_order", "t3_default_tile", "t3_tiles_per_chunk", "t3_tile_of",
                   "t3_track_reset", "t3_gemm_rs_fused", "t3_gemm", "t3_rs_reduce",
                   "t3_upstream_update", "t3_release_chunks", "t3_gemm_rs_fused_static",
-                  "t3_ag_step", "t3_timeline"):
+                  "t3_ag_step", "t3_timeline", "t3_quant_rows", "t3_gemm_i8", "t3_gemm_rs_fused_i8",
+                  "t3_gemm_grouped", "t3_gemm_grouped_i8", "t3_gemm_grouped_wgrad"):
             getattr(L, f).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -108,6 +127,14 @@ def problem(M, N, K, tp, rank, tile_m=0, tile_n=0, b_layout=T3_B_NK, lda=None, l
                      (K if b_layout == T3_B_NK else N) if ldb is None else ldb,
                      N if ldr is None else ldr, N if ldc is None else ldc, tile_limit, flags,
                      tile_begin, split_k, upstream_agents, a_layout, 0)
+
+
+def grouped(rows, groups, N, K, b_layout=T3_B_NK, lda=None, ldb=None, ldc=None, stride_b=None,
+            flags=0):
+    kn = b_layout == T3_B_KN
+    ldb = (N if kn else K) if ldb is None else ldb
+    return T3Grouped(rows, groups, N, K, b_layout, flags, K if lda is None else lda, ldb,
+                     N if ldc is None else ldc, (K if kn else N) * ldb if stride_b is None else stride_b)
 
 
 def _dptr(t):
@@ -217,6 +244,39 @@ def t3_timeline(stamps):
 def t3_gemm(p, A, B, C, stream=None):
     _check(lib().t3_gemm(p, _dptr(A), _dptr(B), _dptr(C), _stream(stream)),
            "t3_gemm")
+
+
+def t3_quant_rows(rows, cols, x, q, scale, ldx=None, ldq=None, x_type=None, stream=None):
+    if x_type is None:                             # a tensor's own type
+        x_type = T3_TYPE_F32 if str(getattr(x, "dtype", "")) == "torch.float32" else T3_TYPE_BF16
+    _check(lib().t3_quant_rows(rows, cols, x_type, _dptr(x), cols if ldx is None else ldx, _dptr(q),
+                               cols if ldq is None else ldq, _dptr(scale), _stream(stream)),
+           "t3_quant_rows")
+
+
+def t3_gemm_i8(p, A, scale_a, B, scale_b, C, stream=None):
+    _check(lib().t3_gemm_i8(p, _dptr(A), _dptr(scale_a), _dptr(B), _dptr(scale_b), _dptr(C),
+                            _stream(stream)), "t3_gemm_i8")
+
+
+def t3_gemm_rs_fused_i8(p, A, scale_a, B, scale_b, R, fwd, track, stream=None):
+    _check(lib().t3_gemm_rs_fused_i8(p, _dptr(A), _dptr(scale_a), _dptr(B), _dptr(scale_b), _dptr(R),
+                                     _dptr(fwd), _dptr(track), _stream(stream)), "t3_gemm_rs_fused_i8")
+
+
+def t3_gemm_grouped(g, offsets, A, B, C, stream=None):
+    _check(lib().t3_gemm_grouped(g, _dptr(offsets), _dptr(A), _dptr(B), _dptr(C), _stream(stream)),
+           "t3_gemm_grouped")
+
+
+def t3_gemm_grouped_i8(g, offsets, A, scale_a, B, scale_b, C, stream=None):
+    _check(lib().t3_gemm_grouped_i8(g, _dptr(offsets), _dptr(A), _dptr(scale_a), _dptr(B),
+                                    _dptr(scale_b), _dptr(C), _stream(stream)), "t3_gemm_grouped_i8")
+
+
+def t3_gemm_grouped_wgrad(g, offsets, A, dC, dB, stream=None):
+    _check(lib().t3_gemm_grouped_wgrad(g, _dptr(offsets), _dptr(A), _dptr(dC), _dptr(dB),
+                                       _stream(stream)), "t3_gemm_grouped_wgrad")
 
 
 def t3_rs_reduce(p, C, R, fwd, track, stream=None):

@@ -10,7 +10,7 @@ LIB = os.path.join(HERE, "libt3.so")
 BUILD_DIR = os.path.join(HERE, "_build")
 # Translation units: (source, object, defines).  t3_gemm_launch.hip is compiled once per mode (0 plain
 # GEMM, 1 fused) and operand layout, so that the kernel instantiations compile in parallel.
-UNITS = [("t3_api.hip", "t3_api.o", [])] + [
+UNITS = [("t3_api.hip", "t3_api.o", []), ("t3_i8_launch.hip", "t3_i8_launch.o", []), ("t3_grouped_launch.hip", "t3_grouped_launch.o", [])] + [
     ("t3_gemm_launch.hip", f"{fn}.o",
      [f"-DT3_LAUNCHER={fn}", f"-DT3_MODE={mode}", f"-DT3_BKN={kn}", f"-DT3_AKM={km}"])
     for fn, mode, kn, km in [
@@ -30,7 +30,7 @@ UNITS = [("t3_api.hip", "t3_api.o", [])] + [
         ("launch_wide_gemm_nk", 0, 0, 0, 0), ("launch_wide_gemm_kn", 0, 1, 0, 0),
         ("launch_wide_gemm_km", 0, 0, 1, 0), ("launch_wide_gemm_km_kn", 0, 1, 1, 0)]]
 DEPS = ["t3_api.hip", "t3_gemm_launch.hip", "t3_small_launch.hip", "t3_wide_launch.hip", "t3_choice.h", "t3_div.h", "t3_device.h", "t3_gemm.h",
-        "t3_small.h", "t3_wide.h", "t3_aux.h", "t3_launch.h"]
+        "t3_small.h", "t3_wide.h", "t3_aux.h", "t3_launch.h", "t3_i8_launch.hip", "t3_grouped_launch.hip", "t3_groups.h", "t3_quant.h"]
 JOBS = 8
 
 HIPCC_FLAGS = [

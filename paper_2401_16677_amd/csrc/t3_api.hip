@@ -12,7 +12,9 @@
 
 #include "t3_aux.h"
 #include "t3_choice.h"
+#include "t3_groups.h"
 #include "t3_launch.h"
+#include "t3_quant.h"
 
 namespace t3k {
 thread_local int32_t last_hip_error = 0;
@@ -264,7 +266,7 @@ inline uint32_t *tail_flags_in(uint32_t *track, int32_t tp) { return track + 2 *
 // Validates everything and fills the plan.  *empty is set when there is nothing to launch.
 t3_status make_plan(const t3_problem *p, t3k::Call call, int need, const void *A, const void *B, const float *C,
                     float *R, void *fwd, uint32_t *track, t3k::Plan *plan, int32_t *tm,
-                    int32_t *tn, bool *empty) {
+                    int32_t *tn, bool *empty, bool i8 = false) {
   t3_status st = check_shape(p);
   if (st != T3_OK) return st;
   st = resolve_tile(p, tm, tn);
@@ -341,7 +343,7 @@ t3_status make_plan(const t3_problem *p, t3k::Call call, int need, const void *A
     st = device_facts(&dev);
     if (st != T3_OK) return st;
   }
-  const t3k::LaunchShape shape = t3k::launch_shape(p, call, {*tm, *tn}, dev.cus);
+  const t3k::LaunchShape shape = t3k::launch_shape(p, call, {*tm, *tn}, dev.cus, i8);
   *tm = shape.tile.m;
   *tn = shape.tile.n;
   const int64_t Mt = shape.Mt, Wt = shape.Wt, tpc = shape.tpc;
@@ -479,6 +481,102 @@ t3_status launch_gemm(int mode, const t3k::Plan &q, int32_t tm, int32_t tn, bool
               : (b_kn ? launch_gemm_kn(q, tm, tn, s) : launch_gemm_nk(q, tm, tn, s));
 }
 
+// ---- products in 8 bits
+constexpr int32_t kMaxK8 = 131056;     // (K of 131072 times -128 -128 is 2^31)
+inline bool aligned4(const void *q) { return (reinterpret_cast<uintptr_t>(q) & 3u) == 0; }
+
+// What a call in 8 bits has to check beside make_plan, and the problem as make_plan takes it: A and B in pairs of int8, which are where
+// a bf16 would be.
+t3_status pairs_of(const t3_problem *p, bool fused, const float *scale_a, const float *scale_b, t3_problem *pairs) {
+  t3_status st = check_shape(p);
+  if (st != T3_OK) return st;
+  if (!scale_a || !scale_b) return T3_ERR_NULL;
+  int32_t tm, tn;
+  st = resolve_tile(p, &tm, &tn);
+  if (st != T3_OK) return st;
+  if ((p->a_layout != T3_A_MK && p->a_layout != T3_A_KM) || (p->b_layout != T3_B_NK && p->b_layout != T3_B_KN)) return T3_ERR_BAD_SHAPE;
+  if (p->a_layout != T3_A_MK || p->b_layout != T3_B_NK) return T3_ERR_UNSUPPORTED;
+  if (fused && ((p->flags & T3_FLAG_TWO_WRITERS) || p->split_k > 1)) return T3_ERR_UNSUPPORTED;
+  if (p->lda < p->K || p->ldb < p->K) return T3_ERR_BAD_SHAPE;
+  if (p->K % 16 || p->lda % 16 || p->ldb % 16 || !aligned4(scale_a) || !aligned4(scale_b)) return T3_ERR_ALIGN;
+  if (p->K > kMaxK8) return T3_ERR_UNSUPPORTED;
+  // ranges of whole ring steps (a range that cuts one is in tracked tiles, which the kernels here do not work in)
+  const int64_t tpc = ceil_div(p->M, tm) * ceil_div(p->N / p->tp, tn), T = tpc * p->tp;
+  const int64_t limit = p->tile_limit < 0 || p->tile_limit > T ? T : p->tile_limit, begin = p->tile_begin < 0 ? 0 : p->tile_begin;
+  if (tpc && begin < limit && (begin % tpc || limit % tpc)) return T3_ERR_UNSUPPORTED;
+  *pairs = *p;
+  pairs->K /= 2;
+  pairs->lda /= 2;
+  pairs->ldb /= 2;
+  return T3_OK;
+}
+
+// ---- products by group
+// The sizes of a grouped product's operands, and what has to hold for them.  size: bytes of an element of A and of B (of dC, in the
+// gradient of the weights, whose result is fp32 in B's place).
+t3_status check_grouped(const t3_grouped *g, bool wgrad, int size) {
+  if (!g) return T3_ERR_NULL;
+  if (g->rows < 0 || g->groups < 1 || g->N < 0 || g->K < 0) return T3_ERR_BAD_SHAPE;
+  if (g->b_layout != T3_B_NK && g->b_layout != T3_B_KN) return T3_ERR_BAD_SHAPE;
+  const bool kn = g->b_layout == T3_B_KN;
+  const int64_t b_rows = kn ? g->K : g->N, b_cols = kn ? g->N : g->K;
+  if (g->lda < g->K || g->ldb < b_cols || g->ldc < g->N || g->stride_b < 0) return T3_ERR_BAD_SHAPE;
+  if (wgrad && g->groups > 1 && b_rows && g->stride_b < (b_rows - 1) * g->ldb + b_cols) return T3_ERR_BAD_SHAPE;
+  if (g->flags & ~(wgrad ? T3_GROUPED_ACCUMULATE : 0u)) return T3_ERR_UNSUPPORTED;
+  if (g->groups > T3_MAX_GROUPS || (size == 1 && (kn || g->K > kMaxK8))) return T3_ERR_UNSUPPORTED;
+  const int per = 16 / size;                     // elements of 16 bytes
+  if (g->K % per || g->lda % per) return T3_ERR_ALIGN;
+  if (wgrad) {
+    if (g->N % 8 || g->ldc % 8 || g->ldb % 4 || g->stride_b % 4) return T3_ERR_ALIGN;
+  } else {
+    if (g->ldb % per || g->stride_b % per || g->N % 4 || g->ldc % 4 || (kn && g->N % 8)) return T3_ERR_ALIGN;
+  }
+  // 32-bit offsets in the kernels: A and a group's B (and dC) below 2^32 bytes and 2^31 elements of 2 bytes, fp32 results below 2^32 bytes
+  // (B's in the gradient of a group)
+  if (g->rows * g->lda >= (1ll << 32) / size || g->rows * g->ldc >= (wgrad ? 1ll << 31 : 1ll << 30) || b_rows * g->ldb >= (wgrad ? 1ll << 30 : (1ll << 32) / size))
+    return T3_ERR_UNSUPPORTED;
+  // tiles, 32 x 32 the smallest, fit 31 bits
+  const int64_t most = wgrad ? ceil_div(b_rows, 32) * ceil_div(b_cols, 32) * g->groups : (ceil_div(g->rows, 32) + g->groups) * ceil_div(g->N, 32);
+  if (most >= (1ll << 31) - 8) return T3_ERR_UNSUPPORTED;
+  return T3_OK;
+}
+
+static_assert(T3_MAX_GROUPS == t3k::kMaxGroups, "groups of the header and of the kernels");
+
+t3_status grouped_product(const t3_grouped *g, bool i8, const int32_t *offsets, const void *A, const float *scale_a, const void *B,
+                          const float *scale_b, float *C, void *stream) {
+  t3_status st = check_grouped(g, false, i8 ? 1 : 2);
+  if (st != T3_OK) return st;
+  if (!offsets || !A || !B || !C || (i8 && (!scale_a || !scale_b))) return T3_ERR_NULL;
+  if (!aligned4(offsets) || !aligned16(A) || !aligned16(B) || !aligned16(C) || (i8 && (!aligned4(scale_a) || !aligned4(scale_b)))) return T3_ERR_ALIGN;
+  if (!g->rows || !g->N) return T3_OK;
+  const int per = i8 ? 2 : 1;
+  t3k::Plan q{};
+  q.A = static_cast<const uint16_t *>(A);
+  q.B = static_cast<const uint16_t *>(B);
+  q.R = C;
+  q.lda = g->lda / per;
+  q.ldb = g->ldb / per;
+  q.ldr = q.ldc = g->ldc;
+  q.M = q.rows = g->rows;
+  q.N = q.W = g->N;
+  q.K = g->K / per;
+  q.P = 1;
+  q.split_k = 1;
+  q.scale_a = scale_a;
+  q.scale_b = scale_b;
+  q.offsets = offsets;
+  q.stride_b = g->stride_b / per;
+  q.groups = g->groups;
+  const int32_t tm = g->rows > 32 * g->groups ? 64 : 32, tn = tm;
+  q.Wt = (int32_t)ceil_div(g->N, tn);
+  // rows of tiles: every group may end with a tile of its own that is not full, and has no more tiles than rows
+  const int64_t ends = g->rows < g->groups ? g->rows : g->groups;
+  q.total_blocks = (int32_t)((ceil_div(g->rows, tm) + ends) * q.Wt + 7) / 8 * 8;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return i8 ? t3k::launch_small_grouped_i8(q, tm, tn, s) : t3k::launch_small_grouped(q, tm, tn, g->b_layout == T3_B_KN, s);
+}
+
 }  // namespace
 
 extern "C" {
@@ -611,6 +709,95 @@ t3_status t3_gemm(const t3_problem *p, const void *A, const void *B, float *C, v
   const bool b_kn = p->b_layout == T3_B_KN, a_km = p->a_layout == T3_A_KM;
   auto go = [&](const t3k::Plan &plan) { return launch_gemm(t3k::kModeGemm, plan, tm, tn, b_kn, a_km, s); };
   return q.tail_r ? launch_with_gemm_tail(q, s, go) : go(q);
+}
+
+t3_status t3_quant_rows(int32_t rows, int32_t cols, int32_t x_type, const void *x, int64_t ldx, int8_t *q, int64_t ldq, float *scale,
+                        void *stream) {
+  if (rows < 0 || cols < 0 || (x_type != T3_TYPE_BF16 && x_type != T3_TYPE_F32) || ldx < cols || ldq < cols) return T3_ERR_BAD_SHAPE;
+  if (!x || !q || !scale) return T3_ERR_NULL;
+  const bool f32 = x_type == T3_TYPE_F32;
+  if (cols % 8 || ldx % (f32 ? 4 : 8) || ldq % 8 || !aligned16(x) || (reinterpret_cast<uintptr_t>(q) & 7u) || !aligned4(scale)) return T3_ERR_ALIGN;
+  if (!rows) return T3_OK;
+  // a wavefront per row, a workgroup where a row is more than a wavefront holds
+  const bool wave = cols <= 8 * 64 * t3k::kQuantPieces;
+  auto kernel = wave ? (f32 ? t3k::quant_rows_kernel<64, true> : t3k::quant_rows_kernel<64, false>)
+                     : (f32 ? t3k::quant_rows_kernel<256, true> : t3k::quant_rows_kernel<256, false>);
+  return launch(kernel, dim3((unsigned)(wave ? ceil_div(rows, 4) : rows)), dim3(256), static_cast<hipStream_t>(stream), x, ldx, q, ldq, scale,
+                rows, cols);
+}
+
+t3_status t3_gemm_i8(const t3_problem *p, const int8_t *A, const float *scale_a, const int8_t *B, const float *scale_b, float *C,
+                     void *stream) {
+  t3_problem pairs;
+  t3_status st = pairs_of(p, false, scale_a, scale_b, &pairs);
+  if (st != T3_OK) return st;
+  t3k::Plan q;
+  int32_t tm, tn;
+  bool empty = false;
+  st = make_plan(&pairs, t3k::kCallGemm, kNeedAB | kNeedC, A, B, C, nullptr, nullptr, nullptr, &q, &tm, &tn, &empty, true);
+  if (st != T3_OK || empty) return st;
+  q.R = C;
+  q.scale_a = scale_a;
+  q.scale_b = scale_b;
+  return t3k::launch_small_gemm_i8(q, tm, tn, static_cast<hipStream_t>(stream));
+}
+
+t3_status t3_gemm_rs_fused_i8(const t3_problem *p, const int8_t *A, const float *scale_a, const int8_t *B, const float *scale_b, float *R,
+                              void *fwd, uint32_t *track, void *stream) {
+  t3_problem pairs;
+  t3_status st = pairs_of(p, true, scale_a, scale_b, &pairs);
+  if (st != T3_OK) return st;
+  t3k::Plan q;
+  int32_t tm, tn;
+  bool empty = false;
+  st = make_plan(&pairs, t3k::kCallFused, kNeedAB | kNeedR | kNeedFwd | kNeedTrack, A, B, nullptr, R, fwd, track, &q, &tm, &tn, &empty, true);
+  if (st != T3_OK || empty) return st;
+  q.scale_a = scale_a;
+  q.scale_b = scale_b;
+  return t3k::launch_small_fused_i8(q, tm, tn, static_cast<hipStream_t>(stream));
+}
+
+t3_status t3_gemm_grouped(const t3_grouped *g, const int32_t *offsets, const void *A, const void *B, float *C, void *stream) {
+  return grouped_product(g, false, offsets, A, nullptr, B, nullptr, C, stream);
+}
+
+t3_status t3_gemm_grouped_i8(const t3_grouped *g, const int32_t *offsets, const int8_t *A, const float *scale_a, const int8_t *B,
+                             const float *scale_b, float *C, void *stream) {
+  return grouped_product(g, true, offsets, A, scale_a, B, scale_b, C, stream);
+}
+
+t3_status t3_gemm_grouped_wgrad(const t3_grouped *g, const int32_t *offsets, const void *A, const void *dC, float *dB, void *stream) {
+  t3_status st = check_grouped(g, true, 2);
+  if (st != T3_OK) return st;
+  if (!offsets || !A || !dC || !dB) return T3_ERR_NULL;
+  if (!aligned4(offsets) || !aligned16(A) || !aligned16(dC) || !aligned16(dB)) return T3_ERR_ALIGN;
+  if (!g->N || !g->K) return T3_OK;
+  const bool kn = g->b_layout == T3_B_KN;        // the result's rows are the columns of: A (else dC)
+  t3k::Plan q{};
+  q.A = static_cast<const uint16_t *>(kn ? A : dC);
+  q.B = static_cast<const uint16_t *>(kn ? dC : A);
+  q.R = dB;
+  q.lda = kn ? g->lda : g->ldc;
+  q.ldb = kn ? g->ldc : g->lda;
+  q.ldr = q.ldc = g->ldb;
+  q.M = kn ? g->K : g->N;
+  q.N = q.W = kn ? g->N : g->K;
+  q.rows = g->rows;
+  q.P = 1;
+  q.split_k = 1;
+  q.offsets = offsets;
+  q.stride_b = g->stride_b;
+  q.groups = g->groups;
+  q.accumulate = g->flags & T3_GROUPED_ACCUMULATE ? 1 : 0;
+  const int64_t tiles64 = ceil_div(q.M, 64) * ceil_div(q.N, 64) * g->groups;
+  const int32_t tm = tiles64 >= kDefaultCus ? 64 : 32, tn = tm;
+  q.Mt = (int32_t)ceil_div(q.M, tm);
+  q.Wt = (int32_t)ceil_div(q.N, tn);
+  q.tpc = q.Mt * q.Wt;
+  q.by_tpc = t3k::fast_div((uint32_t)q.tpc);
+  q.by_column = t3k::fast_div((uint32_t)q.Mt);
+  q.total_blocks = (int32_t)(((int64_t)q.tpc * g->groups + 7) / 8 * 8);
+  return t3k::launch_small_wgrad(q, tm, tn, static_cast<hipStream_t>(stream));
 }
 
 t3_status t3_rs_reduce(const t3_problem *p, const float *C, float *R, void *fwd,

@@ -39,7 +39,8 @@ struct Choice {
 // its LDS stages, gemm_tile_kernel takes its place on the shapes it has: the same main loop rate (12288 x 4096 x 6144,
 // B stored K x N: 493 us, 495 wide), but the incoming partial is waited for at the start of every tile
 // (12288 x 4096 x 1536: 19 us per tile outside the main loop, 14 wide).
-inline Choice workgroup_tile(const t3_problem *p, int cus, int64_t steps, bool wide_ok) {
+// i8: operands in 8 bits, K in pairs of them: as many bytes a slab, as many products in as many clocks; no general kernel.
+inline Choice workgroup_tile(const t3_problem *p, int cus, int64_t steps, bool wide_ok, bool i8 = false) {
   struct Cand {
     TileShape t;
     int stages, per_cu;          // LDS stages of the wide-tile kernel (0: small-tile kernel); workgroups per compute unit
@@ -56,7 +57,8 @@ inline Choice workgroup_tile(const t3_problem *p, int cus, int64_t steps, bool w
   Choice pick{kSmallTile, kCand[5].t};
   for (const Cand &c : kCand) {
     const bool general = c.stages && (!wide_ok || slabs < c.stages);
-    if (general && c.t.n == 192) continue;
+    if (general && (c.t.n == 192 || i8)) continue;
+    if (i8 && c.stages) continue;
     // (32 x 64 is for k-rows of B of a whole 128-byte line; with B K-contiguous two 32 x 32 workgroups take its place
     // at the same time per slab, and start and end sooner)
     if (c.t.m == 32 && c.t.n == 64 && !kn) continue;
@@ -184,7 +186,7 @@ struct LaunchShape {
   int64_t resident;              // workgroups of this tile the device holds at once
   int64_t tail_r, tail_q;        // balanced tail: tiles split, full rounds before them (0: none)
 };
-inline LaunchShape launch_shape(const t3_problem *p, Call call, TileShape tracked, int cus) {
+inline LaunchShape launch_shape(const t3_problem *p, Call call, TileShape tracked, int cus, bool i8 = false) {
   LaunchShape s{};
   const bool two_writers = (call == kCallFused || call == kCallOther) && (p->flags & T3_FLAG_TWO_WRITERS);
   const int64_t W = p->N / p->tp;
@@ -202,7 +204,7 @@ inline LaunchShape launch_shape(const t3_problem *p, Call call, TileShape tracke
     if (call == kCallReduce) {
       s.tile = reduce_tile_shape(p, cus, steps);
     } else {
-      const Choice c = workgroup_tile(p, cus, steps, wide_fits(p, call == kCallGemm ? p->ldc : p->ldr));
+      const Choice c = workgroup_tile(p, cus, steps, wide_fits(p, call == kCallGemm ? p->ldc : p->ldr), i8);
       s.kernel = c.kernel;
       s.tile = c.tile;
     }

@@ -85,6 +85,20 @@ __device__ __forceinline__ void asm_tie(bf16x8 (&a)[6]) {
 __device__ __forceinline__ void asm_tie(bf16x8 (&a)[4]) {
   asm volatile("" : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]));
 }
+// One product of 16 x 16 x 32 bf16, or x 64 int8 (the same bytes of operands in the same lanes).
+typedef __attribute__((ext_vector_type(4))) int i32x4;
+__device__ __forceinline__ f32x4 product(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ i32x4 product(bf16x8 a, bf16x8 b, i32x4 c) {
+  return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
+}
+// Four columns of a row of int8's integer sums, in units of their scales, added to `in`.  (The sums are exact; as floats,
+// times the row's scale, and times the column's with the addition they are rounded once each.)
+__device__ __forceinline__ f32x4 scaled(i32x4 sum, float row, f32x4 column, f32x4 in) {
+  f32x4 v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf((float)sum[e] * row, column[e], in[e]);
+  return v;
+}
 constexpr int kRingSlots = 4;         // 1-KiB LDS slots per wavefront for transposing pairs: two pairs
 
 // WAVES_M x WAVES_N wavefronts per workgroup, each producing a (BM/WAVES_M) x (BN/WAVES_N)

@@ -1,0 +1,27 @@
+// Launches of the products by group.
+#include "t3_small.h"
+#include "t3_launch.h"
+
+namespace t3k {
+namespace {
+
+template <int MODE, int BKN, int AKM, int I8>
+t3_status launch_small(const Plan &q, int32_t tm, int32_t tn, hipStream_t s) {
+  const dim3 grid((unsigned)q.total_blocks), block(256);
+  if (tm == 64 && tn == 64) return launch(small_tile_kernel<64, 64, 4, 2, MODE, BKN, AKM, false, I8>, grid, block, s, q);
+  return tm == 32 && tn == 32 ? launch(small_tile_kernel<32, 32, 4, 2, MODE, BKN, AKM, false, I8>, grid, block, s, q) : T3_ERR_UNSUPPORTED;
+}
+
+}  // namespace
+
+t3_status launch_small_grouped(const Plan &q, int32_t tm, int32_t tn, bool b_kn, hipStream_t s) {
+  return b_kn ? launch_small<kModeGrouped, 1, 0, 0>(q, tm, tn, s) : launch_small<kModeGrouped, 0, 0, 0>(q, tm, tn, s);
+}
+t3_status launch_small_grouped_i8(const Plan &q, int32_t tm, int32_t tn, hipStream_t s) {
+  return launch_small<kModeGrouped, 0, 0, 1>(q, tm, tn, s);
+}
+t3_status launch_small_wgrad(const Plan &q, int32_t tm, int32_t tn, hipStream_t s) {
+  return launch_small<kModeWgrad, 1, 1, 0>(q, tm, tn, s);
+}
+
+}  // namespace t3k

@@ -1,0 +1,110 @@
+// Rows sorted by group: which rows, and which tile, of which group a workgroup has.
+//
+// The groups' sizes are known on the device alone (offsets, written by whatever routed the rows), so a workgroup
+// finds its tile itself: a lane per group has where the group's rows end and how many rows of tiles there are up to
+// and with it, by two scans over the lanes; the group of tile t is the number of groups that end before t.  One request
+// and about sixty instructions at the start of a workgroup; after that a tile is a comparison and a few reads of lanes away.
+//
+// Offsets are taken as they should be: below 0 as 0, past the rows as their number, below the one before as that one.
+// So no group has a row outside of A, no row is in two groups, and there are at most rows / BM + groups rows of tiles.
+#pragma once
+
+#include "t3_device.h"
+
+namespace t3k {
+
+constexpr int kMaxGroups = 256;
+
+struct GroupTile {
+  int group, row0, rows;               // the group, its first row, how many it has
+  int mi, nj;                          // row and column of the tile in the group
+};
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp(uint32_t old, uint32_t v) {      // (lanes without a source, and rows not in the mask: old)
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)old, (int)v, CTRL, ROWS, 0xf, false);
+}
+// Inclusive scans over the 64 lanes: shifts inside rows of 16 lanes, then the rows' last lanes on to the rows behind.
+template <typename Op>
+__device__ __forceinline__ uint32_t lane_scan(uint32_t v, Op op) {        // (0 is neutral)
+  v = op(v, dpp<0x111, 0xf>(0u, v));
+  v = op(v, dpp<0x112, 0xf>(0u, v));
+  v = op(v, dpp<0x114, 0xf>(0u, v));
+  v = op(v, dpp<0x118, 0xf>(0u, v));
+  v = op(v, dpp<0x142, 0xa>(0u, v));
+  return op(v, dpp<0x143, 0xc>(0u, v));
+}
+
+struct GroupRows {
+  static constexpr int kSets = kMaxGroups / 64;
+  uint32_t end[kSets], tiles[kSets];   // lane l of set r, group 64 r + l: behind its last row; rows of tiles up to and with it
+  uint32_t first, all_tiles;           // first row of the first group; rows of tiles of all groups
+
+  template <int BM>
+  __device__ __forceinline__ void load(const Plan &p, int lane) {
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(p.offsets, (uint32_t)(p.groups + 1) * 4u);
+    auto offset = [&](int i) {                   // (past the array's end 0: no rows)
+      return (uint32_t)min(max((int)__builtin_amdgcn_raw_buffer_load_b32(r, i * 4, 0, 0), 0), p.rows);
+    };
+    uint32_t v[kSets];
+    const uint32_t v0 = offset(0);
+#pragma unroll
+    for (int s = 0; s < kSets; ++s) v[s] = s == 0 || p.groups > 64 * s ? offset(64 * s + lane + 1) : 0u;
+    first = __builtin_amdgcn_readfirstlane(v0);
+    uint32_t before = first, count = 0u;
+#pragma unroll
+    for (int s = 0; s < kSets; ++s) {
+      end[s] = before;
+      tiles[s] = count;
+      if (s == 0 || p.groups > 64 * s) {
+        const uint32_t e = lane_scan(max(v[s], before), [](uint32_t a, uint32_t b) { return max(a, b); });
+        const uint32_t rows = e - dpp<0x138, 0xf>(before, e);               // (the lane before's; lane 0: the set before's last)
+        const uint32_t t = lane_scan((rows + BM - 1) / BM, [](uint32_t a, uint32_t b) { return a + b; }) + count;
+        end[s] = e;
+        tiles[s] = t;
+        before = __builtin_amdgcn_readlane(e, 63);
+        count = __builtin_amdgcn_readlane(t, 63);
+      }
+    }
+    all_tiles = count;
+  }
+  __device__ __forceinline__ static uint32_t of(const uint32_t (&a)[kSets], int g) {
+    uint32_t v = __builtin_amdgcn_readlane(a[0], g & 63);
+#pragma unroll
+    for (int s = 1; s < kSets; ++s)
+      if (g >> 6 == s) v = __builtin_amdgcn_readlane(a[s], g & 63);
+    return v;
+  }
+  __device__ __forceinline__ void rows_of(int g, GroupTile &t) const {
+    t.group = g;
+    t.row0 = (int)(g ? of(end, g - 1) : first);
+    t.rows = (int)of(end, g) - t.row0;
+  }
+  // Tile at grid position b of products whose rows are grouped.  Positions are dealt round-robin to the 8 XCDs: each gets a run of
+  // neighbouring tiles (down the columns, which share the group's B), as long as the others' up to one.
+  __device__ __forceinline__ bool tile_at(const Plan &p, uint32_t b, GroupTile &t) const {
+    const uint32_t n = all_tiles * (uint32_t)p.Wt, x = b & 7, i = b >> 3;
+    if (i >= (n >> 3) + (x < (n & 7) ? 1u : 0u)) return false;
+    const uint32_t at = (n >> 3) * x + min(n & 7, x) + i;
+    int g = 0;
+#pragma unroll
+    for (int s = 0; s < kSets; ++s) g += __builtin_popcountll(__ballot(tiles[s] * (uint32_t)p.Wt <= at));
+    rows_of(g, t);
+    const uint32_t before = g ? of(tiles, g - 1) : 0u, Mt = of(tiles, g) - before, q = at - before * (uint32_t)p.Wt;
+    t.nj = (int)(q / Mt);
+    t.mi = (int)(q - (uint32_t)t.nj * Mt);
+    return true;
+  }
+  // ... and of products whose contraction runs over a group's rows: tpc tiles for every group.
+  __device__ __forceinline__ bool tile_of_all(const Plan &p, uint32_t b, GroupTile &t) const {
+    const uint32_t n = (uint32_t)p.groups * (uint32_t)p.tpc, x = b & 7, i = b >> 3;
+    if (i >= (n >> 3) + (x < (n & 7) ? 1u : 0u)) return false;
+    const uint32_t at = (n >> 3) * x + min(n & 7, x) + i, g = div_by(at, p.by_tpc), q = at - g * (uint32_t)p.tpc;
+    rows_of((int)g, t);
+    t.nj = (int)div_by(q, p.by_column);
+    t.mi = (int)(q - (uint32_t)t.nj * (uint32_t)p.Mt);
+    return true;
+  }
+};
+
+}  // namespace t3k

@@ -51,4 +51,13 @@ t3_status launch_wide_gemm_km_kn(const Plan &q, int32_t tm, int32_t tn, hipStrea
 t3_status launch_small_fused(const Plan &q, int32_t tm, int32_t tn, bool b_kn, bool a_km, hipStream_t s);
 t3_status launch_small_gemm(const Plan &q, int32_t tm, int32_t tn, bool b_kn, bool a_km, hipStream_t s);
 
+// The same kernels on operands in 8 bits (t3_i8_launch.hip), A and B K-contiguous.
+t3_status launch_small_fused_i8(const Plan &q, int32_t tm, int32_t tn, hipStream_t s);
+t3_status launch_small_gemm_i8(const Plan &q, int32_t tm, int32_t tn, hipStream_t s);
+
+// Products by group (t3_grouped_launch.hip).
+t3_status launch_small_grouped(const Plan &q, int32_t tm, int32_t tn, bool b_kn, hipStream_t s);
+t3_status launch_small_grouped_i8(const Plan &q, int32_t tm, int32_t tn, hipStream_t s);
+t3_status launch_small_wgrad(const Plan &q, int32_t tm, int32_t tn, hipStream_t s);
+
 }  // namespace t3k

@@ -15,6 +15,7 @@
 #pragma once
 
 #include "t3_gemm.h"
+#include "t3_groups.h"
 
 namespace t3k {
 
@@ -22,7 +23,9 @@ namespace t3k {
 // take the place of finished ones find the lines in the scalar cache, and a request past it costs each of them 0.3 us (by scalar loads and
 // by vector: 24 x 12288 x 1536 on 8 chunks, 384 tiles of 32 x 32, 10.9 us, 10.8; 33 x 16000 x 256 on 2, 250 of 64 x 64,
 // 8.3, 8.1; 24 x 24576 x 1536 on 8, 768 of 32 x 32, 17.1, 17.7; 16 x 24576 x 4096 on 16 41.1, 42.4; 2097 x 1280 x 1472 on 32, 1056 of 64 x 64, 47.5, 48.1).
-template <int BM, int BN, int WK, int NST, int MODE, int BKN, int AKM, bool WORDS>
+// I8: operands in 8 bits, whose sums are integers up to where the incoming partial is added.  MODE kModeGrouped, kModeWgrad: products by
+// group, a tile being one group's.
+template <int BM, int BN, int WK, int NST, int MODE, int BKN, int AKM, bool WORDS, int I8 = 0>
 __global__ __launch_bounds__(64 * WK) void small_tile_kernel(const Plan arg) {
   constexpr int FM = BM / 16, FN = BN / 16, KS = kBK / 32;
   constexpr int NA = BM / kRPC, NB = BN / kRPC, NL = NA + NB;     // 1-KiB copies per slab
@@ -47,12 +50,33 @@ __global__ __launch_bounds__(64 * WK) void small_tile_kernel(const Plan arg) {
     if (MODE == kModeFused) gen = *(const __attribute__((address_space(4))) uint32_t *)(p.track + 2 * trk_bank_words(p.P));
   };
   if (WORDS) ask_generation();
-  Tile tl;
-  if (!decode_block(p, (int)blockIdx.x, tl)) return;
+  constexpr bool grouped = MODE == kModeGrouped, wgrad = MODE == kModeWgrad;
+  Tile tl{0, 0, 0, 0};
+  int row_lo = 0, row_hi = p.M;                  // rows of A and of the result the tile's are among
+  if constexpr (grouped || wgrad) {
+    GroupRows g;
+    g.load<BM>(p, lane);
+    GroupTile at;
+    if (grouped ? !g.tile_at(p, blockIdx.x, at) : !g.tile_of_all(p, blockIdx.x, at)) return;
+    tl = Tile{0, 0, at.mi, at.nj};
+    if (grouped) {
+      row_lo = at.row0;
+      row_hi = at.row0 + at.rows;
+      p.B += at.group * p.stride_b;
+      p.scale_b += (int64_t)at.group * p.N;
+    } else {
+      p.A += at.row0 * p.lda;
+      p.B += at.row0 * p.ldb;
+      p.R += at.group * p.stride_b;
+      p.K = at.rows;
+    }
+  } else {
+    if (!decode_block(p, (int)blockIdx.x, tl)) return;
+  }
   if (!WORDS) ask_generation();
 
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int m0 = tl.mi * BM, col_lo = tl.c * p.W, col_hi = col_lo + p.W, n0 = col_lo + tl.nj * BN;
+  const int m0 = row_lo + tl.mi * BM, col_lo = tl.c * p.W, col_hi = col_lo + p.W, n0 = col_lo + tl.nj * BN;
   const int nkf = p.K / kBK, ktail = p.K - nkf * kBK;
   const int n = wave < nkf ? (nkf - wave + WK - 1) / WK : 0;      // full slabs of this wavefront
 
@@ -76,7 +100,7 @@ __global__ __launch_bounds__(64 * WK) void small_tile_kernel(const Plan arg) {
       tr_at(q, kARowBytes, kSwMaskA, k, col);
       offA[q] = (uint32_t)((k * p.lda + min(m0 + col, p.M - 8)) * 2);
     } else {
-      offA[q] = (uint32_t)((min(m0 + q * kRPC + lane / kCPR, p.M - 1) * p.lda + k_chunk(q) * 8) * 2);
+      offA[q] = (uint32_t)((min(m0 + q * kRPC + lane / kCPR, row_hi - 1) * p.lda + k_chunk(q) * 8) * 2);
     }
   }
 #pragma unroll
@@ -113,11 +137,11 @@ __global__ __launch_bounds__(64 * WK) void small_tile_kernel(const Plan arg) {
   // ---- this wavefront's rows of the tile: the incoming partial, behind the first slabs.  (The
   // waits for slabs below count the slabs' copies only: with these loads among them they wait for
   // a few copies more than they need, never fewer.)
-  const bool store_only = MODE == kModeGemm || ((p.flags & kFlagStep0StoreOnly) && tl.s == 0);
+  const bool store_only = wgrad ? !p.accumulate : MODE != kModeFused || ((p.flags & kFlagStep0StoreOnly) && tl.s == 0);
   const bool direct = MODE == kModeFused && (p.flags & kFlagFwdDirect);
   const bool to_fwd = MODE == kModeFused && tl.c != p.own && (direct || chunk_is_whole(p, tl.s));
   const bool to_out = !direct || tl.c == p.own;
-  const uint32_t ld_out = (uint32_t)(MODE == kModeGemm ? p.ldc : p.ldr);
+  const uint32_t ld_out = (uint32_t)(MODE == kModeFused ? p.ldr : p.ldc);
   const __amdgpu_buffer_rsrc_t r_rsrc = make_rsrc(p.R, (uint32_t)p.M * ld_out * 4u);
   auto at_row = [&](int u) { return wave * kRowsPerWave + (u * 64 + lane) / kChunks; };
   const int chunk = lane % kChunks, col = n0 + chunk * 4;         // (64 is a multiple of kChunks)
@@ -126,8 +150,17 @@ __global__ __launch_bounds__(64 * WK) void small_tile_kernel(const Plan arg) {
   for (int u = 0; u < NIN; ++u) {
     in[u] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int row = m0 + at_row(u);
-    if (!store_only && row < p.M && col < col_hi)
+    if (!store_only && row < row_hi && col < col_hi)
       in[u] = load_stream(r_rsrc, ((uint32_t)row * ld_out + (uint32_t)col) * 4u, 0u);
+  }
+  float scale_a[NIN];
+  f32x4 scale_b;
+  if constexpr (I8) {                            // (past the arrays' ends: zeros)
+    const __amdgpu_buffer_rsrc_t a_rsrc = make_rsrc(p.scale_a, (uint32_t)p.M * 4u), b_rsrc = make_rsrc(p.scale_b, (uint32_t)p.N * 4u);
+#pragma unroll
+    for (int u = 0; u < NIN; ++u)
+      scale_a[u] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(a_rsrc, (m0 + at_row(u)) * 4, 0, 0));
+    scale_b = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(b_rsrc, col * 4, 0, 0));
   }
 
   // ---- K loop
@@ -162,11 +195,12 @@ __global__ __launch_bounds__(64 * WK) void small_tile_kernel(const Plan arg) {
                              : *(const bf16x8 *)(st + kBOff + frag[kk] + j * 16 * kRowBytes);
     }
   };
-  f32x4 acc[FM][FN];
+  using Sum = std::conditional_t<I8, i32x4, f32x4>;
+  Sum acc[FM][FN];
 #pragma unroll
   for (int i = 0; i < FM; ++i)
 #pragma unroll
-    for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < FN; ++j) acc[i][j] = Sum{0, 0, 0, 0};
   auto multiply = [&](auto SET) {
     constexpr int set = decltype(SET)::value;
 #pragma unroll
@@ -175,7 +209,7 @@ __global__ __launch_bounds__(64 * WK) void small_tile_kernel(const Plan arg) {
       for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[set][kk][j], fa[set][kk][i], acc[i][j], 0, 0, 0);
+          acc[i][j] = product(fb[set][kk][j], fa[set][kk][i], acc[i][j]);
   };
   auto wait_slabs = [&](int younger) {            // at most `younger` slabs still on their way
     if (NST >= 3 && younger >= 2) __builtin_amdgcn_s_waitcnt(wait_vm(2 * NL));
@@ -207,7 +241,25 @@ __global__ __launch_bounds__(64 * WK) void small_tile_kernel(const Plan arg) {
     }
     if (i < n) step(set0, i);
   }
-  if (ktail && wave == nkf % WK) {                // ragged end of K (K-contiguous operands only)
+  if (ktail && wave == nkf % WK) {                // ragged end of K: K-contiguous operands, and any in products by group
+    if constexpr (wgrad || (grouped && BKN)) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      const char *a = (const char *)p.A + (AKM ? (int64_t)nkf * kBK * p.lda * 2 : (int64_t)nkf * (kBK * 2));
+      const char *b = (const char *)p.B + (int64_t)nkf * kBK * p.ldb * 2;
+#pragma unroll
+      for (int q = 0; q < NL; ++q) {
+        const int r = q < NA ? q : q - NA;
+        int k, col;
+        tr_at(r, q < NA ? kARowBytes : kBRowBytes, 0, k, col);
+        if (q < NA && !AKM) k = k_chunk(r) * 8;
+        u32x4 v{0, 0, 0, 0};
+        if (k < ktail) v = *(const __attribute__((address_space(1))) u32x4 *)(q < NA ? a + offA[q < NA ? q : 0] : b + offB[q < NA ? 0 : r]);
+        *(u32x4 *)(st0 + q * 1024 + lane * 16) = v;
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      read_slab(set0, st0);
+      multiply(set0);
+    }
     if constexpr (!AKM && !BKN) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       const int64_t kb = (int64_t)nkf * (kBK * 2);
@@ -234,7 +286,7 @@ __global__ __launch_bounds__(64 * WK) void small_tile_kernel(const Plan arg) {
     for (int i = 0; i < FM; ++i)
 #pragma unroll
       for (int j = 0; j < FN; ++j)
-        *(f32x4 *)(mine + (16 * i + fr) * (BN * 4) + (((4 * j + fq) ^ (fr & 7)) << 4)) = acc[i][j];
+        *(Sum *)(mine + (16 * i + fr) * (BN * 4) + (((4 * j + fq) ^ (fr & 7)) << 4)) = acc[i][j];
   }
   __syncthreads();
   const float *slot = p.fwd + (int64_t)tl.s * p.M * p.W;
@@ -245,11 +297,15 @@ __global__ __launch_bounds__(64 * WK) void small_tile_kernel(const Plan arg) {
 #pragma unroll
   for (int u = 0; u < NIN; ++u) {
     const int r = at_row(u), row = m0 + r;
-    f32x4 v = in[u];
+    Sum sum = Sum{0, 0, 0, 0};
+    if constexpr (!I8) sum = in[u];
 #pragma unroll
     for (int w = 0; w < WK; ++w)
-      v += *(const f32x4 *)(lds + w * (BM * BN * 4) + r * (BN * 4) + ((chunk ^ (r & 7)) << 4));
-    if (row < p.M && col < col_hi) {
+      sum += *(const Sum *)(lds + w * (BM * BN * 4) + r * (BN * 4) + ((chunk ^ (r & 7)) << 4));
+    f32x4 v;
+    if constexpr (I8) v = scaled(sum, scale_a[u], scale_b, in[u]);
+    else v = sum;
+    if (row < row_hi && col < col_hi) {
       if (to_out) store_agent(r_rsrc, ((uint32_t)row * ld_out + (uint32_t)col) * 4u, 0u, v);
       const uint32_t at = (uint32_t)row * (uint32_t)p.W + (uint32_t)(col - col_lo);
       if (to_fwd && !bf16) store_agent(f_rsrc, at * 4u, 0u, v);

@@ -1,0 +1,116 @@
+"""Arguments of the products in 8 bits and by group that are refused before anything is launched; no GPU needed."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from paper_2401_16677_amd import binding as t3
+from products import rows8, spans
+
+FAKE = 0x10000
+
+
+def status(call, *args):
+    try:
+        call(*args, stream=0)
+    except t3.T3Error as e:
+        return e.status
+    return t3.T3_OK
+
+
+def quant(rows=4, cols=64, x=FAKE, q=FAKE, s=FAKE, ldx=None, ldq=None, x_type=t3.T3_TYPE_BF16):
+    return status(lambda **k: t3.t3_quant_rows(rows, cols, x, q, s, ldx=ldx, ldq=ldq, x_type=x_type, **k))
+
+
+def test_rows_refused():
+    assert quant(rows=0) == t3.T3_OK
+    assert quant(x=None) == quant(q=None) == quant(s=None) == t3.T3_ERR_NULL
+    assert quant(rows=-1) == quant(cols=-8) == quant(ldx=56) == quant(ldq=56) == quant(x_type=2) == t3.T3_ERR_BAD_SHAPE
+    assert quant(cols=60, ldx=64, ldq=64) == quant(ldx=68) == quant(ldq=68) == quant(x=FAKE + 2) == quant(q=FAKE + 4) == quant(s=FAKE + 2) == t3.T3_ERR_ALIGN
+    assert quant(ldx=66, x_type=t3.T3_TYPE_F32) == t3.T3_ERR_ALIGN
+
+
+GEMM = dict(M=256, N=1024, K=256, tp=4, rank=0, tile_m=128, tile_n=128)
+
+
+def plain(A=FAKE, sa=FAKE, B=FAKE, sb=FAKE, C=FAKE, **kw):
+    return status(t3.t3_gemm_i8, t3.problem(**{**GEMM, **kw}), A, sa, B, sb, C)
+
+
+def fused(A=FAKE, sa=FAKE, B=FAKE, sb=FAKE, R=FAKE, fwd=FAKE, track=FAKE, **kw):
+    return status(t3.t3_gemm_rs_fused_i8, t3.problem(**{**GEMM, **kw}), A, sa, B, sb, R, fwd, track)
+
+
+@pytest.mark.parametrize("call", [plain, fused])
+def test_products_in_8_bits_refused(call):
+    assert call(M=0) == call(N=0) == t3.T3_OK
+    assert call(A=None) == call(sa=None) == call(B=None) == call(sb=None) == t3.T3_ERR_NULL
+    assert call(M=-1) == call(rank=4) == call(N=1022) == call(lda=240) == call(ldb=240) == call(a_layout=2) == call(b_layout=2) == t3.T3_ERR_BAD_SHAPE
+    assert call(tile_m=96) == t3.T3_ERR_BAD_TILE
+    assert call(K=248) == call(lda=264) == call(ldb=264) == call(A=FAKE + 8) == call(B=FAKE + 8) == call(sa=FAKE + 2) == call(sb=FAKE + 1) == t3.T3_ERR_ALIGN
+    assert call(b_layout=t3.T3_B_KN, ldb=1024) == call(a_layout=t3.T3_A_KM, lda=256) == call(K=131072) == t3.T3_ERR_UNSUPPORTED
+    assert call(tile_begin=1) == call(tile_limit=5) == t3.T3_ERR_UNSUPPORTED      # (16 tiles a ring step)
+    assert call(M=1 << 20, K=4096) == t3.T3_ERR_UNSUPPORTED                        # A of 2^32 bytes
+    lib = t3.lib()
+    assert lib.t3_gemm_i8(None, FAKE, FAKE, FAKE, FAKE, FAKE, 0) == t3.T3_ERR_NULL
+    assert lib.t3_gemm_rs_fused_i8(None, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 0) == t3.T3_ERR_NULL
+
+
+def test_results_of_products_in_8_bits_refused():
+    assert plain(C=None) == fused(R=None) == fused(fwd=None) == fused(track=None) == t3.T3_ERR_NULL
+    assert plain(ldc=1000) == fused(ldr=1000) == t3.T3_ERR_BAD_SHAPE
+    assert plain(ldc=1026) == plain(C=FAKE + 4) == fused(R=FAKE + 4) == fused(N=1016) == t3.T3_ERR_ALIGN
+    assert fused(flags=t3.T3_FLAG_TWO_WRITERS) == fused(flags=16) == fused(split_k=2) == t3.T3_ERR_UNSUPPORTED
+
+
+GROUPED = dict(rows=100, groups=4, N=64, K=128)
+
+
+def grouped(o=FAKE, A=FAKE, B=FAKE, C=FAKE, **kw):
+    return status(t3.t3_gemm_grouped, t3.grouped(**{**GROUPED, **kw}), o, A, B, C)
+
+
+def grouped8(o=FAKE, A=FAKE, sa=FAKE, B=FAKE, sb=FAKE, C=FAKE, **kw):
+    return status(t3.t3_gemm_grouped_i8, t3.grouped(**{**GROUPED, **kw}), o, A, sa, B, sb, C)
+
+
+def wgrad(o=FAKE, A=FAKE, B=FAKE, C=FAKE, **kw):
+    return status(t3.t3_gemm_grouped_wgrad, t3.grouped(**{**GROUPED, **kw}), o, A, C, B)
+
+
+@pytest.mark.parametrize("call", [grouped, grouped8, wgrad])
+def test_groups_refused(call):
+    assert call(o=None) == call(A=None) == call(B=None) == call(C=None) == t3.T3_ERR_NULL
+    assert call(rows=-1) == call(groups=0) == call(N=-4) == call(K=-8) == call(b_layout=2) == t3.T3_ERR_BAD_SHAPE
+    assert call(lda=120) == call(ldb=120) == call(ldc=60) == call(stride_b=-8) == t3.T3_ERR_BAD_SHAPE
+    assert call(groups=257) == call(flags=2) == t3.T3_ERR_UNSUPPORTED
+    assert call(K=124) == call(N=62) == call(lda=130) == call(ldc=66) == call(ldb=130) == call(stride_b=64 * 128 + 2) == t3.T3_ERR_ALIGN
+    assert call(o=FAKE + 2) == call(A=FAKE + 8) == call(B=FAKE + 8) == call(C=FAKE + 8) == t3.T3_ERR_ALIGN
+    assert call(rows=1 << 25, K=256) == call(rows=1 << 25, N=64, ldc=128) == t3.T3_ERR_UNSUPPORTED or call is grouped8
+    assert call(N=0) == t3.T3_OK
+
+
+def test_groups_refused_by_one_call():
+    assert grouped(b_layout=t3.T3_B_KN, K=100) == grouped(b_layout=t3.T3_B_KN, N=60) == t3.T3_ERR_ALIGN
+    assert grouped(flags=t3.T3_GROUPED_ACCUMULATE) == grouped8(flags=t3.T3_GROUPED_ACCUMULATE) == t3.T3_ERR_UNSUPPORTED
+    assert grouped8(b_layout=t3.T3_B_KN) == grouped8(K=131072) == grouped8(rows=1 << 25, K=128) == t3.T3_ERR_UNSUPPORTED
+    assert grouped8(sa=None) == grouped8(sb=None) == t3.T3_ERR_NULL
+    assert grouped8(K=120) == grouped8(lda=136) == grouped8(sa=FAKE + 2) == grouped8(sb=FAKE + 2) == t3.T3_ERR_ALIGN
+    assert wgrad(stride_b=64 * 128 - 4) == wgrad(stride_b=0) == t3.T3_ERR_BAD_SHAPE     # groups' results over one another
+    assert wgrad(N=60, ldc=64) == wgrad(K=120, lda=124, ldb=128) == t3.T3_ERR_ALIGN
+    assert grouped(rows=0) == grouped8(rows=0) == wgrad(K=0) == t3.T3_OK
+    lib = t3.lib()
+    assert lib.t3_gemm_grouped(None, FAKE, FAKE, FAKE, FAKE, 0) == t3.T3_ERR_NULL
+    assert lib.t3_gemm_grouped_i8(None, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 0) == t3.T3_ERR_NULL
+    assert lib.t3_gemm_grouped_wgrad(None, FAKE, FAKE, FAKE, FAKE, 0) == t3.T3_ERR_NULL
+
+
+def test_struct_layout():
+    assert ctypes.sizeof(t3.T3Grouped) == 6 * 4 + 4 * 8 and t3.T3Grouped.lda.offset == 24 and t3.T3Grouped.stride_b.offset == 48
+
+
+def test_the_tests_own_reading_of_rows_and_offsets():
+    q, s = rows8(np.array([[127.0, 0.5, 1.5, -2.5], [0, 0, 0, 0], [np.nan, 1, 1, 1]]))
+    assert q.tolist() == [[127, 0, 2, -2], [0] * 4, [0] * 4] and s[0] == 1.0 and s[1] == 0.0 and np.isnan(s[2])
+    assert spans([5, 2, 30, 30], 40) == [(5, 5), (5, 30), (30, 30)]
+    assert spans([-4, 10, 2000000000, 3], 25) == [(0, 10), (10, 25), (25, 25)]
