@@ -541,6 +541,20 @@ t3_status check_grouped(const t3_grouped *g, bool wgrad, int size) {
   return T3_OK;
 }
 
+// What the launches of products by group have in common: how grid positions fall to the workgroups.
+void plan_rounds(t3k::Plan &q, const t3k::Choice &c, const DeviceFacts &dev, int64_t most_tiles) {
+  q.tile_m = c.tile.m;
+  q.tile_n = c.tile.n;
+  q.wide = c.kernel == t3k::kWideTile;
+  q.Wt = (int32_t)ceil_div(q.N, c.tile.n);
+  q.resident = dev.cus * (c.tile.m == 128 && c.tile.n == 128 ? 2 : 1);
+  q.order.round = (uint32_t)q.resident;
+  q.order.by_round = t3k::fast_div(q.order.round);
+  q.total_blocks = (int32_t)((most_tiles + 7) / 8 * 8);
+  q.k_groups = dev.xcds > 1 ? dev.xcds : 0;
+  q.by_groups = t3k::fast_div((uint32_t)(q.k_groups > 1 ? q.k_groups : 1));
+}
+
 static_assert(T3_MAX_GROUPS == t3k::kMaxGroups, "groups of the header and of the kernels");
 
 t3_status grouped_product(const t3_grouped *g, bool i8, const int32_t *offsets, const void *A, const float *scale_a, const void *B,
@@ -568,13 +582,20 @@ t3_status grouped_product(const t3_grouped *g, bool i8, const int32_t *offsets, 
   q.offsets = offsets;
   q.stride_b = g->stride_b / per;
   q.groups = g->groups;
-  const int32_t tm = g->rows > 32 * g->groups ? 64 : 32, tn = tm;
-  q.Wt = (int32_t)ceil_div(g->N, tn);
+  const bool kn = g->b_layout == T3_B_KN;
+  DeviceFacts dev;
+  st = device_facts(&dev);
+  if (st != T3_OK) return st;
+  // (the wide-tile kernel's limits, see wide_fits)
+  const bool wide_ok = 256 * q.lda * 2 <= 1ll << 31 && (kn ? q.K : 256) * q.ldb * 2 <= 1ll << 31 && 256 * q.ldc * 4 <= 1ll << 31;
+  const t3k::Choice c = t3k::grouped_tile(false, kn, g->rows, g->N, q.K, g->groups, dev.cus, wide_ok);
+  const int32_t tm = c.tile.m, tn = c.tile.n;
   // rows of tiles: every group may end with a tile of its own that is not full, and has no more tiles than rows
-  const int64_t ends = g->rows < g->groups ? g->rows : g->groups;
-  q.total_blocks = (int32_t)((ceil_div(g->rows, tm) + ends) * q.Wt + 7) / 8 * 8;
+  plan_rounds(q, c, dev, (ceil_div(g->rows, tm) + (g->rows < g->groups ? g->rows : g->groups)) * ceil_div(g->N, tn));
   hipStream_t s = static_cast<hipStream_t>(stream);
-  return i8 ? t3k::launch_small_grouped_i8(q, tm, tn, s) : t3k::launch_small_grouped(q, tm, tn, g->b_layout == T3_B_KN, s);
+  if (q.wide)
+    return i8 ? t3k::launch_wide_grouped_i8(q, tm, tn, s) : (kn ? t3k::launch_wide_grouped_kn(q, tm, tn, s) : t3k::launch_wide_grouped_nk(q, tm, tn, s));
+  return i8 ? t3k::launch_small_grouped_i8(q, tm, tn, s) : t3k::launch_small_grouped(q, tm, tn, kn, s);
 }
 
 }  // namespace
@@ -739,7 +760,10 @@ t3_status t3_gemm_i8(const t3_problem *p, const int8_t *A, const float *scale_a,
   q.R = C;
   q.scale_a = scale_a;
   q.scale_b = scale_b;
-  return t3k::launch_small_gemm_i8(q, tm, tn, static_cast<hipStream_t>(stream));
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  q.ldr = q.ldc;                                 // (C through R)
+  auto go = [&](const t3k::Plan &plan) { return plan.wide ? t3k::launch_wide_gemm_i8(plan, tm, tn, s) : t3k::launch_small_gemm_i8(plan, tm, tn, s); };
+  return q.tail_r ? launch_with_gemm_tail(q, s, go) : go(q);
 }
 
 t3_status t3_gemm_rs_fused_i8(const t3_problem *p, const int8_t *A, const float *scale_a, const int8_t *B, const float *scale_b, float *R,
@@ -754,7 +778,9 @@ t3_status t3_gemm_rs_fused_i8(const t3_problem *p, const int8_t *A, const float 
   if (st != T3_OK || empty) return st;
   q.scale_a = scale_a;
   q.scale_b = scale_b;
-  return t3k::launch_small_fused_i8(q, tm, tn, static_cast<hipStream_t>(stream));
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (!q.wide) return t3k::launch_small_fused_i8(q, tm, tn, s);
+  return q.overlap ? t3k::launch_wide_overlap_i8(q, tm, tn, s) : t3k::launch_wide_fused_i8(q, tm, tn, s);
 }
 
 t3_status t3_gemm_grouped(const t3_grouped *g, const int32_t *offsets, const void *A, const void *B, float *C, void *stream) {
@@ -789,15 +815,20 @@ t3_status t3_gemm_grouped_wgrad(const t3_grouped *g, const int32_t *offsets, con
   q.stride_b = g->stride_b;
   q.groups = g->groups;
   q.accumulate = g->flags & T3_GROUPED_ACCUMULATE ? 1 : 0;
-  const int64_t tiles64 = ceil_div(q.M, 64) * ceil_div(q.N, 64) * g->groups;
-  const int32_t tm = tiles64 >= kDefaultCus ? 64 : 32, tn = tm;
+  DeviceFacts dev;
+  st = device_facts(&dev);
+  if (st != T3_OK) return st;
+  // (the wide-tile kernel's limits, see wide_fits: a group's rows, and the slabs of zeros behind them)
+  const int64_t k_rows = (int64_t)g->rows + 4 * 64;
+  const bool wide_ok = k_rows * q.lda * 2 <= 1ll << 31 && k_rows * q.ldb * 2 <= 1ll << 31 && 256 * q.ldc * 4 <= 1ll << 31;
+  const t3k::Choice c = t3k::grouped_tile(true, true, q.M, q.N, g->rows, g->groups, dev.cus, wide_ok);
+  const int32_t tm = c.tile.m, tn = c.tile.n;
   q.Mt = (int32_t)ceil_div(q.M, tm);
-  q.Wt = (int32_t)ceil_div(q.N, tn);
-  q.tpc = q.Mt * q.Wt;
+  q.tpc = q.Mt * (int32_t)ceil_div(q.N, tn);
   q.by_tpc = t3k::fast_div((uint32_t)q.tpc);
-  q.by_column = t3k::fast_div((uint32_t)q.Mt);
-  q.total_blocks = (int32_t)(((int64_t)q.tpc * g->groups + 7) / 8 * 8);
-  return t3k::launch_small_wgrad(q, tm, tn, static_cast<hipStream_t>(stream));
+  plan_rounds(q, c, dev, (int64_t)q.tpc * g->groups);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return q.wide ? t3k::launch_wide_wgrad(q, tm, tn, s) : t3k::launch_small_wgrad(q, tm, tn, s);
 }
 
 t3_status t3_rs_reduce(const t3_problem *p, const float *C, float *R, void *fwd,

@@ -40,16 +40,16 @@ struct Choice {
 // B stored K x N: 493 us, 495 wide), but the incoming partial is waited for at the start of every tile
 // (12288 x 4096 x 1536: 19 us per tile outside the main loop, 14 wide).
 // i8: operands in 8 bits, K in pairs of them: as many bytes a slab, as many products in as many clocks; no general kernel.
+struct Cand {
+  TileShape t;
+  int stages, per_cu;            // LDS stages of the wide-tile kernel (0: small-tile kernel); workgroups per compute unit
+  double slab_us, ends_us;       // a K-slab of 64 / the rest of a tile
+};
+constexpr Cand kCand[] = {{{256, 256}, 2, 1, 1.22, 14.3}, {{256, 192}, 2, 1, 0.90, 13.3},
+                          {{256, 128}, 3, 1, 0.75, 10.9}, {{128, 192}, 3, 1, 0.59, 8.2},
+                          {{128, 128}, 2, 2, 0.81, 7.4},  {{64, 64}, 0, 1, 0.166, 6.55},
+                          {{32, 64}, 0, 1, 0.113, 6.9},   {{32, 32}, 0, 2, 0.115, 5.3}};
 inline Choice workgroup_tile(const t3_problem *p, int cus, int64_t steps, bool wide_ok, bool i8 = false) {
-  struct Cand {
-    TileShape t;
-    int stages, per_cu;          // LDS stages of the wide-tile kernel (0: small-tile kernel); workgroups per compute unit
-    double slab_us, ends_us;     // a K-slab of 64 / the rest of a tile
-  };
-  static const Cand kCand[] = {{{256, 256}, 2, 1, 1.22, 14.3}, {{256, 192}, 2, 1, 0.90, 13.3},
-                               {{256, 128}, 3, 1, 0.75, 10.9}, {{128, 192}, 3, 1, 0.59, 8.2},
-                               {{128, 128}, 2, 2, 0.81, 7.4},  {{64, 64}, 0, 1, 0.166, 6.55},
-                               {{32, 64}, 0, 1, 0.113, 6.9},   {{32, 32}, 0, 2, 0.115, 5.3}};
   const bool km = p->a_layout == T3_A_KM, kn = p->b_layout == T3_B_KN;
   const int64_t W = p->N / p->tp;
   const int64_t slabs = ceil_div(p->K, 64);
@@ -58,7 +58,6 @@ inline Choice workgroup_tile(const t3_problem *p, int cus, int64_t steps, bool w
   for (const Cand &c : kCand) {
     const bool general = c.stages && (!wide_ok || slabs < c.stages);
     if (general && (c.t.n == 192 || i8)) continue;
-    if (i8 && c.stages) continue;
     // (32 x 64 is for k-rows of B of a whole 128-byte line; with B K-contiguous two 32 x 32 workgroups take its place
     // at the same time per slab, and start and end sooner)
     if (c.t.m == 32 && c.t.n == 64 && !kn) continue;
@@ -75,6 +74,31 @@ inline Choice workgroup_tile(const t3_problem *p, int cus, int64_t steps, bool w
     if (best < 0 || us < best * 0.999) {
       best = us;
       pick = {!c.stages ? kSmallTile : (general ? kGeneralTile : kWideTile), c.t};
+    }
+  }
+  return pick;
+}
+
+// The tile of products by group, by the same times.  The host knows the rows of all groups together, so the tiles are those of groups
+// as large as the average, every one with half a tile more than its rows fill (or one tile), and the rounds those of tiles that fill the
+// last one half.  M x N: C, or the gradient of a group's weights (wgrad), whose K is a group's rows.
+inline Choice grouped_tile(bool wgrad, bool kn, int64_t M, int64_t N, int64_t K, int64_t groups, int cus, bool wide_ok) {
+  double best = -1.0;
+  Choice pick{kSmallTile, {64, 64}};
+  for (const Cand &c : kCand) {
+    if (c.t.m == 32 && c.t.n == 64) continue;
+    const double used = (double)(wgrad || M > groups ? groups : M), columns = (double)ceil_div(N, c.t.n);
+    const double even = (double)M / c.t.m + 0.5 * used;
+    const double T = (wgrad ? (double)(groups * ceil_div(M, c.t.m)) : (even > used ? even : used)) * columns, slots = (double)cus * c.per_cu;
+    double slabs = wgrad ? (double)K / ((double)groups * 64.0) + 0.5 : (double)ceil_div(K, 64);
+    if (c.stages && (!wide_ok || (!wgrad && slabs < c.stages))) continue;
+    if (slabs < c.stages) slabs = c.stages;
+    const double rounds = T <= slots ? 1.0 : T / slots + 0.5, alone = c.per_cu == 2 && T <= cus ? 0.8 : 1.0;
+    const double slab_us = c.slab_us * (wgrad && c.t.m == 32 ? 1.34 : 1.0) * ((wgrad || kn) && c.t.n == 32 ? 1.34 : 1.0);
+    const double us = rounds * alone * (c.ends_us + slab_us * slabs);
+    if (best < 0 || us < best * 0.999) {
+      best = us;
+      pick = {c.stages ? kWideTile : kSmallTile, c.t};
     }
   }
   return pick;

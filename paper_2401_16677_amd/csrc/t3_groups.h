@@ -80,29 +80,40 @@ struct GroupRows {
     t.row0 = (int)(g ? of(end, g - 1) : first);
     t.rows = (int)of(end, g) - t.row0;
   }
-  // Tile at grid position b of products whose rows are grouped.  Positions are dealt round-robin to the 8 XCDs: each gets a run of
-  // neighbouring tiles (down the columns, which share the group's B), as long as the others' up to one.
+  // Grid position b of n tiles.  Workgroups are dealt round-robin to the 8 XCDs: of every round of positions each XCD gets a run of
+  // neighbouring tiles, as long as the others' up to one.
+  __device__ __forceinline__ static bool place(const Plan &p, uint32_t b, uint32_t n, uint32_t &at) {
+    const uint32_t base = div_by(b, p.order.by_round) * p.order.round, j = b - base, x = j & 7;
+    if (base >= n) return false;
+    const uint32_t here = min(n - base, p.order.round), odd = here & 7;
+    at = base + (here >> 3) * x + min(odd, x) + (j >> 3);
+    return (j >> 3) < (here >> 3) + (x < odd ? 1u : 0u);
+  }
+  // Tile q of a group's Mt x Wt: columns four at a time, row by row, so that a run of tiles shares both rows and columns.
+  __device__ __forceinline__ static void in_group(uint32_t q, uint32_t Mt, uint32_t Wt, GroupTile &t) {
+    const uint32_t band = q / (4u * Mt), in = q - band * 4u * Mt, width = min(4u, Wt - 4u * band), row = in / width;
+    t.mi = (int)row;
+    t.nj = (int)(4u * band + in - row * width);
+  }
+  // Tile at grid position b of products whose rows are grouped
   __device__ __forceinline__ bool tile_at(const Plan &p, uint32_t b, GroupTile &t) const {
-    const uint32_t n = all_tiles * (uint32_t)p.Wt, x = b & 7, i = b >> 3;
-    if (i >= (n >> 3) + (x < (n & 7) ? 1u : 0u)) return false;
-    const uint32_t at = (n >> 3) * x + min(n & 7, x) + i;
+    uint32_t at;
+    if (!place(p, b, all_tiles * (uint32_t)p.Wt, at)) return false;
     int g = 0;
 #pragma unroll
     for (int s = 0; s < kSets; ++s) g += __builtin_popcountll(__ballot(tiles[s] * (uint32_t)p.Wt <= at));
     rows_of(g, t);
     const uint32_t before = g ? of(tiles, g - 1) : 0u, Mt = of(tiles, g) - before, q = at - before * (uint32_t)p.Wt;
-    t.nj = (int)(q / Mt);
-    t.mi = (int)(q - (uint32_t)t.nj * Mt);
+    in_group(q, Mt, (uint32_t)p.Wt, t);
     return true;
   }
   // ... and of products whose contraction runs over a group's rows: tpc tiles for every group.
   __device__ __forceinline__ bool tile_of_all(const Plan &p, uint32_t b, GroupTile &t) const {
-    const uint32_t n = (uint32_t)p.groups * (uint32_t)p.tpc, x = b & 7, i = b >> 3;
-    if (i >= (n >> 3) + (x < (n & 7) ? 1u : 0u)) return false;
-    const uint32_t at = (n >> 3) * x + min(n & 7, x) + i, g = div_by(at, p.by_tpc), q = at - g * (uint32_t)p.tpc;
+    uint32_t at;
+    if (!place(p, b, (uint32_t)p.groups * (uint32_t)p.tpc, at)) return false;
+    const uint32_t g = div_by(at, p.by_tpc);
     rows_of((int)g, t);
-    t.nj = (int)div_by(q, p.by_column);
-    t.mi = (int)(q - (uint32_t)t.nj * (uint32_t)p.Mt);
+    in_group(at - g * (uint32_t)p.tpc, (uint32_t)p.Mt, (uint32_t)p.Wt, t);
     return true;
   }
 };

@@ -54,10 +54,17 @@ t3_status launch_small_gemm(const Plan &q, int32_t tm, int32_t tn, bool b_kn, bo
 // The same kernels on operands in 8 bits (t3_i8_launch.hip), A and B K-contiguous.
 t3_status launch_small_fused_i8(const Plan &q, int32_t tm, int32_t tn, hipStream_t s);
 t3_status launch_small_gemm_i8(const Plan &q, int32_t tm, int32_t tn, hipStream_t s);
+t3_status launch_wide_fused_i8(const Plan &q, int32_t tm, int32_t tn, hipStream_t s);        // (t3_wide_products_launch.hip)
+t3_status launch_wide_overlap_i8(const Plan &q, int32_t tm, int32_t tn, hipStream_t s);
+t3_status launch_wide_gemm_i8(const Plan &q, int32_t tm, int32_t tn, hipStream_t s);
 
 // Products by group (t3_grouped_launch.hip).
 t3_status launch_small_grouped(const Plan &q, int32_t tm, int32_t tn, bool b_kn, hipStream_t s);
 t3_status launch_small_grouped_i8(const Plan &q, int32_t tm, int32_t tn, hipStream_t s);
 t3_status launch_small_wgrad(const Plan &q, int32_t tm, int32_t tn, hipStream_t s);
+t3_status launch_wide_grouped_nk(const Plan &q, int32_t tm, int32_t tn, hipStream_t s);      // (t3_wide_products_launch.hip)
+t3_status launch_wide_grouped_kn(const Plan &q, int32_t tm, int32_t tn, hipStream_t s);
+t3_status launch_wide_grouped_i8(const Plan &q, int32_t tm, int32_t tn, hipStream_t s);
+t3_status launch_wide_wgrad(const Plan &q, int32_t tm, int32_t tn, hipStream_t s);
 
 }  // namespace t3k

@@ -27,10 +27,14 @@
 // written; no access is conditional, so the number of accesses in flight is always known.  (Addresses past the
 // buffer: behind its last row, or kOob = 2^31 plus anything, with buffers of at most 2^31 bytes: the host sees to that.)
 //
+// The same kernel multiplies operands in 8 bits (I8: as many bytes a slab, 16 x 16 x 64 a product; the integer sums become floats times
+// their scales on the way out) and rows sorted by group (MODE kModeGrouped, kModeWgrad: see t3_groups.h; a piece of work is a tile of one group).
+//
 // Included by the launch units only.
 #pragma once
 
 #include "t3_gemm.h"
+#include "t3_groups.h"
 
 namespace t3k {
 
@@ -43,7 +47,8 @@ __device__ __forceinline__ void asm_tie(u32x2 (&a)[6]) {
 __device__ __forceinline__ void asm_tie(u32x2 (&a)[4]) {
   asm volatile("" : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]));
 }
-__device__ __forceinline__ void asm_accumulator(f32x4 &v) { asm volatile("" : "+a"(v)); }
+template <typename Sum>
+__device__ __forceinline__ void asm_accumulator(Sum &v) { asm volatile("" : "+a"(v)); }
 template <int OFF>
 __device__ __forceinline__ void asm_ds_read_tr(u32x2 &dst, uint32_t addr) {
   asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(dst) : "v"(addr), "n"(OFF));
@@ -80,6 +85,7 @@ struct Piece {
   Tile tl;
   int k0, nf, ns;      // first K-slab, full slabs, slabs with a ragged last one
   int half, idx;       // 0: whole tile, 1 / 2: first / second half of split tile idx
+  int row0, rows;      // products by group: the rows of the tile's group (tl.s), tl.c being 0
 };
 // (each part of it reads of the plan what it needs: what is read is read, and kept, whether the branch is taken or not)
 __device__ __forceinline__ bool get_piece(PlanWords &words, int it, Piece &w) {
@@ -106,7 +112,27 @@ __device__ __forceinline__ bool get_piece(PlanWords &words, int it, Piece &w) {
   return true;
 }
 
-template <int FM, int FN, int NSTAGE, int NIMG, int PRE, int DEPTH, int MODE, int BKN, int AKM, int OVERLAP>
+// Products by group.  (As many slabs as there are stages at least: behind a group's rows they are zeros.)
+template <int MODE, int BM, int NSTAGE>
+__device__ __forceinline__ bool get_group_piece(PlanWords &words, const GroupRows &groups, int it, Piece &w) {
+  const Plan p = words.now();
+  GroupTile at;
+  const uint32_t pos = blockIdx.x + (uint32_t)it * (uint32_t)p.resident;
+  if (MODE == kModeGrouped ? !groups.tile_at(p, pos, at) : !groups.tile_of_all(p, pos, at)) return false;
+  w.tl = Tile{at.group, 0, at.mi, at.nj};
+  w.k0 = w.half = w.idx = 0;
+  w.row0 = at.row0;
+  w.rows = at.rows;
+  if (MODE == kModeGrouped) {
+    w.nf = p.K / kBK;
+    w.ns = w.nf + (p.K % kBK ? 1 : 0);
+  } else {
+    w.nf = w.ns = max((at.rows + kBK - 1) / kBK, NSTAGE);
+  }
+  return true;
+}
+
+template <int FM, int FN, int NSTAGE, int NIMG, int PRE, int DEPTH, int MODE, int BKN, int AKM, int OVERLAP, int I8 = 0>
 __global__ __launch_bounds__(256)
 __attribute__((amdgpu_waves_per_eu((32 * (FM + FN) * 128 * NSTAGE + NIMG * 4096 * FN) <= 80 * 1024 ? 2 : 1)))
 void wide_tile_kernel(const Plan) {
@@ -119,11 +145,17 @@ void wide_tile_kernel(const Plan) {
   static_assert(PRE > 0 && PRE <= DEPTH && DEPTH <= FM && NL + PRE * FN < 64, "");
   __shared__ __attribute__((aligned(1024))) char lds[kImgOff + NIMG * kImgBytes];
 
-  constexpr bool tracked = MODE == kModeFused;
+  constexpr bool tracked = MODE == kModeFused, grouped = MODE == kModeGrouped, wgrad = MODE == kModeWgrad;
   const int lane = threadIdx.x & 63;
   PlanWords words;
   words.load(lane);
   Plan p = words.now();                          // (read anew where something rare begins)
+  GroupRows groups;
+  if constexpr (grouped || wgrad) groups.load<BM>(p, lane);
+  auto piece_of = [&](int it, Piece &w) {
+    if constexpr (grouped || wgrad) return get_group_piece<MODE, BM, NSTAGE>(words, groups, it, w);
+    else return get_piece(words, it, w);
+  };
   // The tracker's generation, a scalar load nothing waits for until a tile is counted.  (Waited for here it puts a round trip
   // to memory in front of the first slabs.)  It is read as constant memory, which it is while this workgroup reads it: the launch's
   // end, which changes it, waits for every workgroup's last count.
@@ -238,12 +270,19 @@ void wide_tile_kernel(const Plan) {
   };
   Walk walkA, walkB;
   auto stream_to = [&](const Piece &w) {
-    const int m0 = w.tl.mi * BM, at = col_at(w.tl), n0 = w.tl.c * p.W + at;
-    const int rows = min(BM, p.M - m0), cols = cols_of(w.tl, at);
+    const int m0 = (grouped ? w.row0 : 0) + w.tl.mi * BM, at = col_at(w.tl), n0 = w.tl.c * p.W + at;
+    const int rows = min(BM, (grouped ? w.row0 + w.rows : p.M) - m0), cols = cols_of(w.tl, at);
     // (arrays of less than 2^31 elements: offsets in them are 32-bit products)
     const uint32_t lda = (uint32_t)p.lda, ldb = (uint32_t)p.ldb;
+    if constexpr (grouped) p.B += w.tl.s * p.stride_b;
+    if constexpr (wgrad) {                       // (K is the group's rows; of none, buffers of no bytes)
+      p.A += (uint32_t)w.row0 * lda;
+      p.B += (uint32_t)w.row0 * ldb;
+      p.K = w.rows;
+    }
     descA = AKM ? descriptor(p.A + m0, ((uint32_t)p.K * lda - m0) * 2u) : descriptor(p.A + (uint32_t)m0 * lda, (uint32_t)rows * lda * 2u);
     descB = BKN ? descriptor(p.B + n0, ((uint32_t)p.K * ldb - n0) * 2u) : descriptor(p.B + (uint32_t)n0 * ldb, (uint32_t)cols * ldb * 2u);
+    if (wgrad && w.rows == 0) descA[2] = descB[2] = 0u;
     const bool cutA = AKM && rows < BM, cutB = BKN && cols < BN;
     if (cutA || markedA) {
 #pragma unroll
@@ -282,6 +321,12 @@ void wide_tile_kernel(const Plan) {
 #pragma unroll
       for (int q = 0; q < NB; ++q) offB[q] = mark(offB[q], k_chunk(q) * 8 >= ktail);
       markedA = markedB = true;
+    } else if constexpr (grouped) {              // (k-rows of B past the last are past its buffer)
+      walkA.at = walkA.end;
+      walkB.at = walkB.end;
+#pragma unroll
+      for (int q = 0; q < NA; ++q) offA[q] = mark(offA[q], k_chunk(q) * 8 >= ktail);
+      markedA = true;
     }
   };
   auto stream_end = [&]() { descA[2] = descB[2] = 0u; };          // (buffers of no bytes)
@@ -361,7 +406,8 @@ void wide_tile_kernel(const Plan) {
     else
       read_a(std::integral_constant<int, (r - RB * FN) / RA>{}, std::integral_constant<int, (r - RB * FN) % RA>{}, SET, KK, a_addr);
   };
-  f32x4 acc[FM][FN];
+  using Sum = std::conditional_t<I8, i32x4, f32x4>;
+  Sum acc[FM][FN];
   // One k-step: the products of operand set CS, (READS) k-step KK's operands of the stage at `sr` into the
   // other set, and (COPIES) the stream's slab into the stage at `sc`.  `under`: what else is to be done under the products.
   auto kstep = [&](auto FIRST, auto CS, auto KK, auto READS, auto COPIES, uint32_t sr, uint32_t sc, auto under) {
@@ -379,7 +425,7 @@ void wide_tile_kernel(const Plan) {
     __builtin_amdgcn_sched_barrier(0);
     static_for<NP>([&](auto Mi) {
       constexpr int m = decltype(Mi)::value, i = m / FN, j = m % FN;
-      acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xb[cs].template get<j>(), xa[cs].template get<i>(), decltype(FIRST)::value ? f32x4{0.f, 0.f, 0.f, 0.f} : acc[i][j], 0, 0, 0);
+      acc[i][j] = product(xb[cs].template get<j>(), xa[cs].template get<i>(), decltype(FIRST)::value ? Sum{0, 0, 0, 0} : acc[i][j]);
       __builtin_amdgcn_sched_barrier(0);                          // nothing moves across: the order is as written
       if constexpr (m == 0) {
         a_addr = adA[AKM ? 0 : kk] + sr;
@@ -414,7 +460,7 @@ void wide_tile_kernel(const Plan) {
   auto strip_row = [](int ir) { return (ir >> 4) * WM + (ir & 15); };   // image row -> tile row, row block 0
 
   Piece cur;
-  get_piece(words, 0, cur);                      // (the grid is no larger than the number of pieces)
+  if (!piece_of(0, cur) && (grouped || wgrad)) return;             // (else the grid is no larger than the number of pieces)
   p = words.now();
   stream_to(cur);
 #pragma unroll
@@ -442,7 +488,7 @@ void wide_tile_kernel(const Plan) {
     stamp(it, 0);
     const Tile tl = cur.tl;
     p = words.now();
-    const bool has_in = cur.half == 2 || (tracked && !((p.flags & kFlagStep0StoreOnly) && tl.s == 0));
+    const bool has_in = wgrad ? p.accumulate != 0 : cur.half == 2 || (tracked && !((p.flags & kFlagStep0StoreOnly) && tl.s == 0));
 
     if (cur.ns <= NSTAGE) flush();               // (too short a K loop to put the count off into)
     if (cur.half == 2 && wave == 0) {
@@ -485,9 +531,10 @@ void wide_tile_kernel(const Plan) {
     };
     auto place = [&]() {
       Place o;
-      const int m0 = tl.mi * BM, at = col_at(tl), n0 = tl.c * p.W + at;
-      o.rows_in = (uint32_t)min(BM, p.M - m0);
+      const int m0 = (grouped ? cur.row0 : 0) + tl.mi * BM, at = col_at(tl), n0 = tl.c * p.W + at;
+      o.rows_in = (uint32_t)min(BM, (grouped ? cur.row0 + cur.rows : p.M) - m0);
       o.cols_in = cols_of(tl, at);
+      if constexpr (wgrad) p.R += tl.s * p.stride_b;
       const bool direct = (p.flags & kFlagFwdDirect) != 0;
       o.bf16 = (p.flags & kFlagFwdBf16) != 0;
       o.to_slot = tracked && tl.c != p.own && cur.half != 1 && (direct || chunk_is_whole(p, tl.s));
@@ -537,6 +584,24 @@ void wide_tile_kernel(const Plan) {
       inside(o, lane, in);
       offsets(lane, ld_in, 4u, in, in_at);
     };
+    // (I8) The scales of this lane's rows, as the sums are in registers, and of its columns, as they leave: requested with the incoming
+    // partial.  Past the arrays' ends they are zeros.
+    constexpr int kScales = I8 ? FM + UB : 0;
+    float scale_a[FM];
+    f32x4 scale_b[UB];
+    auto load_scales = [&]() {
+      const int m0 = (grouped ? cur.row0 : 0) + tl.mi * BM, n0 = tl.c * p.W + col_at(tl);
+      const float *of_rows = p.scale_a + m0, *of_columns = p.scale_b + ((grouped ? (int64_t)tl.s * p.N : 0) + n0);
+      const __amdgpu_buffer_rsrc_t a_rsrc = make_rsrc(of_rows, (uint32_t)(p.M - m0) * 4u), b_rsrc = make_rsrc(of_columns, (uint32_t)(p.N - n0) * 4u);
+      static_for<FM>([&](auto I) {
+        constexpr int i = decltype(I)::value;
+        scale_a[i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(a_rsrc, (wm * WM + 16 * i + fr) * 4, 0, 0));
+      });
+      static_for<UB>([&](auto U) {
+        constexpr int u = decltype(U)::value;
+        scale_b[u] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(b_rsrc, lane_col(lane, u) * 4, 0, 0));
+      });
+    };
     Piece nxt;
     bool more = false;
     // The K loop.  A slab is two k-steps with a barrier between them, behind which the slab's stage is free and
@@ -567,7 +632,8 @@ void wide_tile_kernel(const Plan) {
     // What it waits for beside them: the next slab's copies, with the incoming partial requested behind them or not; or nothing
     // (the first slabs of every piece but the first landed during the way out, and behind the last slab nothing is needed).
     auto next_landed = [&]() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"((NSTAGE - 2) * NL) : "memory"); };
-    auto next_landed_in = [&]() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"((NSTAGE - 2) * NL + PRE * FN) : "memory"); };
+    auto next_landed_in = [&]() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"((NSTAGE - 2) * NL + PRE * FN + kScales) : "memory"); };
+    auto next_landed_scales = [&]() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"((NSTAGE - 2) * NL + kScales) : "memory"); };
     first_half(true_type{});
     if (it == 0 && last > 0) next_landed();
     barrier();
@@ -578,7 +644,7 @@ void wide_tile_kernel(const Plan) {
         if (kt == NSTAGE) act_on_count();
       }
       if (kt == k_switch) {
-        more = get_piece(words, it + 1, nxt);
+        more = piece_of(it + 1, nxt);
         p = words.now();
         if (more) stream_to(nxt);
         else stream_end();
@@ -587,6 +653,10 @@ void wide_tile_kernel(const Plan) {
           in_here(place());
           static_for<PRE>([&](auto I) { load_in(I); });
         }
+        if constexpr (I8) {
+          p = words.now();
+          load_scales();
+        }
       }
       // the slab copied next is the last one of the stream's piece, and ragged
       if (ktail && (kt == k_switch - 1 || (kt == last && more && nxt.ns == NSTAGE)) && (kt < k_switch ? cur.ns > cur.nf : nxt.ns > nxt.nf))
@@ -594,7 +664,7 @@ void wide_tile_kernel(const Plan) {
       // the next barrier something is to be done behind, or whose wait is another one
       int stop = kt < k_switch ? (ktail && kt < k_switch - 1 ? k_switch - 1 : k_switch) : (NSTAGE > 2 && kt < last - 1 ? kt + 1 : last);
       if (kt < NSTAGE && (counting || (NSTAGE > 2 && it > 0))) stop = min(stop, kt + 1);
-      const int kind = kt + 1 == last || (it > 0 && kt + 1 < NSTAGE - 1) ? 2 : (NSTAGE > 2 && kt >= k_switch && tracked && has_in ? 1 : 0);
+      const int kind = kt + 1 == last || (it > 0 && kt + 1 < NSTAGE - 1) ? 2 : (NSTAGE > 2 && kt >= k_switch && tracked && has_in ? 1 : (I8 && NSTAGE > 2 && kt >= k_switch ? 3 : 0));
       do {
         kstep(false_type{}, c1, c0, true_type{}, true_type{}, sn, so, []() {});     // (behind the last slab it reads what nobody uses)
         so = sn;
@@ -608,6 +678,7 @@ void wide_tile_kernel(const Plan) {
         first_half(false_type{});
         if (kind == 0) next_landed();
         else if (kind == 1) next_landed_in();
+        else if (I8 && kind == 3) next_landed_scales();
         barrier();
       } while (kt < stop);
       if (kt == cur.ns) break;
@@ -624,6 +695,19 @@ void wide_tile_kernel(const Plan) {
     int lane_e = lane;                           // recomputed here rather than kept through the main loop
     asm volatile("" : "+v"(lane_e));
     const int e_row = lane_e & 15, e_q = lane_e >> 4;
+    auto result = [&](auto I, int j) {           // (I8: the sum as a float, times the row's scale)
+      constexpr int i = decltype(I)::value;
+      if constexpr (I8) {
+        Sum sum = acc[i][j];
+        asm volatile("" : "+v"(sum));            // (turned here: all ways out have this in common, and the compiler would turn the whole tile ahead of them)
+        f32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (float)sum[e] * scale_a[i];
+        return v;
+      } else {
+        return acc[i][j];
+      }
+    };
     // TO: -1 = fp32 to C, kept in the caches; 0 = fp32 to R, C or a slot, streamed; 1 = R and the fp32 slot; 2 = the bfloat16 slot; 3 = R and the bfloat16 slot
     // ADD: there is something to add
     auto way_out = [&](auto TO, auto ADD) {
@@ -660,7 +744,7 @@ void wide_tile_kernel(const Plan) {
         }
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
-          *(f32x4 *)(lds + kImgOff + img + (wm * 16 + e_row) * (BN * 4) + (((wn * (WN / 4) + 4 * j + e_q) ^ (e_row & 7)) << 4)) = acc[i][j];
+          *(f32x4 *)(lds + kImgOff + img + (wm * 16 + e_row) * (BN * 4) + (((wn * (WN / 4) + 4 * j + e_q) ^ (e_row & 7)) << 4)) = result(I, j);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
@@ -668,7 +752,13 @@ void wide_tile_kernel(const Plan) {
         static_for<FN>([&](auto U) {
           constexpr int u = decltype(U)::value;
           f32x4 v = *(const f32x4 *)(lds + img + img_at[u]);
-          if constexpr (add) v += in[i][u];
+          if constexpr (I8) {
+            const f32x4 column = scale_b[u % UB];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = add ? __builtin_fmaf(v[e], column[e], in[i][u][e]) : v[e] * column[e];
+          } else if constexpr (add) {
+            v += in[i][u];
+          }
           const uint32_t rows = (uint32_t)(16 * i + (u / UB) * RS);
           if constexpr (kTo != 2) store_agent_hint<(kTo >= 0)>(out_rsrc, out_at[u % UB] + rows * ld_out * 4u, 0u, v);
           if constexpr (kTo == 1) store_agent_hint<true>(slot_rsrc, slot_at[u % UB] + rows * W * 4u, 0u, v);
@@ -698,7 +788,7 @@ void wide_tile_kernel(const Plan) {
       } else {
         way_out(c0, true_type{});
       }
-    } else if (cur.half == 2) {
+    } else if (wgrad ? has_in : cur.half == 2) {
       way_out(keep, true_type{});
     } else {
       if (nt_out) way_out(c0, false_type{});
