@@ -541,8 +541,11 @@ t3_status check_grouped(const t3_grouped *g, bool wgrad, int size) {
   return T3_OK;
 }
 
-// What the launches of products by group have in common: how grid positions fall to the workgroups.
-void plan_rounds(t3k::Plan &q, const t3k::Choice &c, const DeviceFacts &dev, int64_t most_tiles) {
+// What the launches of products by group have in common: how grid positions fall to the workgroups, and whether results leave the caches.
+// bytes: of operands and result.  Results stream where all of it is more than the memory-side cache holds.  In us, kept and streamed,
+// and with a reader of C right behind: 8192 rows of 16 groups x 5120 x 1280, 398 MB, 136 and 105, with the reader 180 and 177; the gradient
+// of its weights, 524 MB, 181 and 137; 16384 of 8 x 8192 x 1024, 705 MB, 298 and 264, 439 and 450; 4096 of 8 x 5120 x 1280, 200 MB, 61 and 59, 79 and 82.
+void plan_rounds(t3k::Plan &q, const t3k::Choice &c, const DeviceFacts &dev, int64_t most_tiles, int64_t bytes) {
   q.tile_m = c.tile.m;
   q.tile_n = c.tile.n;
   q.wide = c.kernel == t3k::kWideTile;
@@ -553,6 +556,7 @@ void plan_rounds(t3k::Plan &q, const t3k::Choice &c, const DeviceFacts &dev, int
   q.total_blocks = (int32_t)((most_tiles + 7) / 8 * 8);
   q.k_groups = dev.xcds > 1 ? dev.xcds : 0;
   q.by_groups = t3k::fast_div((uint32_t)(q.k_groups > 1 ? q.k_groups : 1));
+  q.nt_out = bytes > kMemorySideCacheBytes ? 1 : 0;
 }
 
 static_assert(T3_MAX_GROUPS == t3k::kMaxGroups, "groups of the header and of the kernels");
@@ -591,7 +595,8 @@ t3_status grouped_product(const t3_grouped *g, bool i8, const int32_t *offsets, 
   const t3k::Choice c = t3k::grouped_tile(false, kn, g->rows, g->N, q.K, g->groups, dev.cus, wide_ok);
   const int32_t tm = c.tile.m, tn = c.tile.n;
   // rows of tiles: every group may end with a tile of its own that is not full, and has no more tiles than rows
-  plan_rounds(q, c, dev, (ceil_div(g->rows, tm) + (g->rows < g->groups ? g->rows : g->groups)) * ceil_div(g->N, tn));
+  plan_rounds(q, c, dev, (ceil_div(g->rows, tm) + (g->rows < g->groups ? g->rows : g->groups)) * ceil_div(g->N, tn),
+              2ll * q.rows * q.K + 2ll * q.groups * q.N * q.K + 4ll * q.rows * q.N);
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (q.wide)
     return i8 ? t3k::launch_wide_grouped_i8(q, tm, tn, s) : (kn ? t3k::launch_wide_grouped_kn(q, tm, tn, s) : t3k::launch_wide_grouped_nk(q, tm, tn, s));
@@ -739,10 +744,15 @@ t3_status t3_quant_rows(int32_t rows, int32_t cols, int32_t x_type, const void *
   const bool f32 = x_type == T3_TYPE_F32;
   if (cols % 8 || ldx % (f32 ? 4 : 8) || ldq % 8 || !aligned16(x) || (reinterpret_cast<uintptr_t>(q) & 7u) || !aligned4(scale)) return T3_ERR_ALIGN;
   if (!rows) return T3_OK;
-  // a wavefront per row, a workgroup where a row is more than a wavefront holds
-  const bool wave = cols <= 8 * 64 * t3k::kQuantPieces;
-  auto kernel = wave ? (f32 ? t3k::quant_rows_kernel<64, true> : t3k::quant_rows_kernel<64, false>)
-                     : (f32 ? t3k::quant_rows_kernel<256, true> : t3k::quant_rows_kernel<256, false>);
+  // a wavefront per row of up to four pieces a lane, else a workgroup; as many pieces as the row has
+  const bool wave = cols <= 8 * 64 * 4;
+  const int64_t held = ceil_div(cols, 8 * (wave ? 64 : 256));
+  auto pick = [&](auto type) {
+    constexpr bool kF32 = decltype(type)::value;
+    if (wave) return held <= 1 ? t3k::quant_rows_kernel<64, 1, kF32> : (held <= 2 ? t3k::quant_rows_kernel<64, 2, kF32> : t3k::quant_rows_kernel<64, 4, kF32>);
+    return held <= 2 ? t3k::quant_rows_kernel<256, 2, kF32> : (held <= 4 ? t3k::quant_rows_kernel<256, 4, kF32> : t3k::quant_rows_kernel<256, t3k::kQuantPieces, kF32>);
+  };
+  auto kernel = f32 ? pick(std::true_type{}) : pick(std::false_type{});
   return launch(kernel, dim3((unsigned)(wave ? ceil_div(rows, 4) : rows)), dim3(256), static_cast<hipStream_t>(stream), x, ldx, q, ldq, scale,
                 rows, cols);
 }
@@ -826,7 +836,7 @@ t3_status t3_gemm_grouped_wgrad(const t3_grouped *g, const int32_t *offsets, con
   q.Mt = (int32_t)ceil_div(q.M, tm);
   q.tpc = q.Mt * (int32_t)ceil_div(q.N, tn);
   q.by_tpc = t3k::fast_div((uint32_t)q.tpc);
-  plan_rounds(q, c, dev, (int64_t)q.tpc * g->groups);
+  plan_rounds(q, c, dev, (int64_t)q.tpc * g->groups, 2ll * q.rows * (q.M + q.N) + 4ll * q.groups * q.M * q.N);
   hipStream_t s = static_cast<hipStream_t>(stream);
   return q.wide ? t3k::launch_wide_wgrad(q, tm, tn, s) : t3k::launch_small_wgrad(q, tm, tn, s);
 }

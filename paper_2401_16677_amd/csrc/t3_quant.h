@@ -8,20 +8,39 @@
 
 namespace t3k {
 
-constexpr int kQuantPieces = 8;        // pieces of 8 elements a lane holds
+constexpr int kQuantPieces = 8;        // pieces of 8 elements a lane holds at most
 
-// 127 x / a to the nearest integer, ties to even, as if the quotient were not rounded before.  In fp32, x times 127 / a is off by less
-// than 2^-15 (two roundings of half a step of numbers up to 127); where that could decide, the quotient is taken in fp64, whose rounding cannot: 127 x is exact
-// there, and a quotient that is no odd multiple of 1/2 is at least 2^-33 away from all of them (twice 127 x and an odd multiple of a are
-// multiples of 2^-7 of a's last place where they are that near).
-__device__ __forceinline__ int quantised(float x, float a, float inv, bool tiny) {
-  const float f = x * inv;
-  float n = __builtin_rintf(f);
-  if (tiny || __builtin_fabsf(f - n) > 0.5f - 0x1p-15f) n = (float)__builtin_rint((double)x * 127.0 / (double)a);
-  return (int)n;
+// 127 x / a to the nearest integer, ties to even, as if the quotient were not rounded before: eight of them, in the bytes of two words.
+// inv = 127 / a, rounded.  x inv is off by less than 2^-15 (two roundings of half a step of numbers up to 127), and 1.5 2^23 + x inv has
+// the integer nearest to it in its low bits.  Where 2^-15 could decide, next to k + 1/2, the sign of 127 x - (k + 1/2) a does: 127 x in two
+// numbers p + rest, and p - (k + 1/2) a, a small multiple of a's last place or of x's, without a rounding.
+__device__ __forceinline__ u32x2 quantised(const float (&x)[8], float a, float inv) {
+  constexpr float kWhole = 12582912.0f, kNear = 0.5f - 0x1p-15f;
+  uint32_t n[8];
+  float off = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float f = x[e] * inv, m = f + kWhole;
+    off = fmaxf(off, __builtin_fabsf(f - (m - kWhole)));
+    n[e] = __builtin_bit_cast(uint32_t, m);
+  }
+  if (off > kNear) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float f = x[e] * inv, below = __builtin_floorf(f), at = f - below;
+      const float p = 127.0f * x[e], rest = __builtin_fmaf(127.0f, x[e], -p), past = __builtin_fmaf(-(below + 0.5f), a, p) + rest;
+      const int k = (int)below, up = past > 0.0f || (past == 0.0f && (k & 1)) ? k + 1 : k;
+      if (__builtin_fabsf(at - 0.5f) < 0x1p-14f) n[e] = (uint32_t)up;
+    }
+  }
+  auto four = [](uint32_t b0, uint32_t b1, uint32_t b2, uint32_t b3) {        // low bytes together
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(b3, b2, 0x0c0c0400u), __builtin_amdgcn_perm(b1, b0, 0x0c0c0400u), 0x05040100u);
+  };
+  return u32x2{four(n[0], n[1], n[2], n[3]), four(n[4], n[5], n[6], n[7])};
 }
 
-template <int TEAM, bool F32>
+// PIECES: of 8 elements that a lane holds at a time.
+template <int TEAM, int PIECES, bool F32>
 __global__ __launch_bounds__(256) void quant_rows_kernel(const void *x, int64_t ldx, int8_t *q, int64_t ldq, float *scale, int32_t rows,
                                                          int32_t cols) {
   __shared__ uint32_t tops[4];
@@ -30,10 +49,10 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const void *x, int64_t 
   if (row >= rows) return;                       // (whole wavefronts; a workgroup of one row stays together)
   const char *from = (const char *)x + row * ldx * (F32 ? 4 : 2);
   const int pieces = cols >> 3;
-  float v[kQuantPieces][8];
+  float v[PIECES][8];
   auto load = [&](int base) {
 #pragma unroll
-    for (int u = 0; u < kQuantPieces; ++u) {
+    for (int u = 0; u < PIECES; ++u) {
       const int at = base + u * TEAM + lane;
       u32x4 lo{0, 0, 0, 0}, hi{0, 0, 0, 0};
       if (at < pieces) {
@@ -53,11 +72,11 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const void *x, int64_t 
   };
   // the largest magnitude by its bits: a NaN's and infinity's are larger than any number's
   uint32_t top = 0;
-  constexpr int kHeld = TEAM * kQuantPieces;
+  constexpr int kHeld = TEAM * PIECES;
   for (int base = 0; base == 0 || base < pieces; base += kHeld) {
     load(base);
 #pragma unroll
-    for (int u = 0; u < kQuantPieces; ++u)
+    for (int u = 0; u < PIECES; ++u)
 #pragma unroll
       for (int e = 0; e < 8; ++e) top = max(top, __builtin_bit_cast(uint32_t, v[u][e]) & 0x7FFFFFFFu);
   }
@@ -69,21 +88,22 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const void *x, int64_t 
     top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
   }
   const bool finite = top < 0x7F800000u, any = top != 0u && finite;
-  const float a = __builtin_bit_cast(float, top), inv = __fdiv_rn(127.0f, a);
-  const bool tiny = a < 0x1p-100f;               // (127 / a might be infinite)
-  if (lane == 0) scale[row] = finite ? __fdiv_rn(a, 127.0f) : __builtin_nanf("");
+  const float largest = __builtin_bit_cast(float, top);
+  if (lane == 0) scale[row] = finite ? __fdiv_rn(largest, 127.0f) : __builtin_nanf("");
+  // (rows whose 127 / a or 127 x might not be a float are taken at another power of two, which changes no quotient; elements that would fall
+  // below the smallest float are nowhere near 1/2)
+  const float by = largest < 0x1p-60f ? 0x1p100f : (largest > 0x1p100f ? 0x1p-20f : 1.0f), a = largest * by, inv = __fdiv_rn(127.0f, a);
   int8_t *to = q + row * ldq;
   for (int base = 0; base == 0 || base < pieces; base += kHeld) {
     if (pieces > kHeld) load(base);
 #pragma unroll
-    for (int u = 0; u < kQuantPieces; ++u) {
+    for (int u = 0; u < PIECES; ++u) {
       const int at = base + u * TEAM + lane;
-      u32x2 w{0, 0};
-      if (any) {
+      if (by != 1.0f) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e >> 2] |= ((uint32_t)quantised(v[u][e], a, inv, tiny) & 0xFFu) << (8 * (e & 3));
+        for (int e = 0; e < 8; ++e) v[u][e] *= by;
       }
-      if (at < pieces) ((u32x2 *)to)[at] = w;
+      if (at < pieces) ((u32x2 *)to)[at] = any ? quantised(v[u], a, inv) : u32x2{0, 0};
     }
   }
 }

@@ -760,7 +760,9 @@ void wide_tile_kernel(const Plan) {
             v += in[i][u];
           }
           const uint32_t rows = (uint32_t)(16 * i + (u / UB) * RS);
-          if constexpr (kTo != 2) store_agent_hint<(kTo >= 0)>(out_rsrc, out_at[u % UB] + rows * ld_out * 4u, 0u, v);
+          if constexpr (grouped || wgrad)        // (nobody reads them before the launch has ended)
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), out_rsrc, (int)(out_at[u % UB] + rows * ld_out * 4u), 0, kTo >= 0 ? kAuxNt : 0);
+          else if constexpr (kTo != 2) store_agent_hint<(kTo >= 0)>(out_rsrc, out_at[u % UB] + rows * ld_out * 4u, 0u, v);
           if constexpr (kTo == 1) store_agent_hint<true>(slot_rsrc, slot_at[u % UB] + rows * W * 4u, 0u, v);
           if constexpr (kTo >= 2)
             __builtin_amdgcn_raw_buffer_store_b64(pack_bf16(v), slot_rsrc, (int)(slot_at[u % UB] + rows * W * 2u), 0,
@@ -788,7 +790,10 @@ void wide_tile_kernel(const Plan) {
       } else {
         way_out(c0, true_type{});
       }
-    } else if (wgrad ? has_in : cur.half == 2) {
+    } else if (wgrad && has_in) {
+      if (nt_out) way_out(c0, true_type{});
+      else way_out(keep, true_type{});
+    } else if (!grouped && !wgrad && cur.half == 2) {
       way_out(keep, true_type{});
     } else {
       if (nt_out) way_out(c0, false_type{});
