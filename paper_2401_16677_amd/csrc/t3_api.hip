@@ -79,6 +79,12 @@ t3_status device_facts(DeviceFacts *out) {
 std::atomic<uint64_t *> g_timeline{nullptr};
 std::atomic<int64_t> g_timeline_wgs{0};
 
+void set_timeline(t3k::Plan &q) {
+  q.timeline = g_timeline.load();
+  const int64_t wgs = g_timeline_wgs.load();
+  q.timeline_wgs = (int32_t)(wgs > (1ll << 30) ? (1ll << 30) : wgs);
+}
+
 // Tracker state for t3_gemm_rs_fused_static, the entry point for callers that cannot allocate:
 // one array per device (each GPU the library runs on holds its own copy at its own address
 // until the process ends).  Host code never uses the array's name as an address: the device
@@ -426,11 +432,7 @@ t3_status make_plan(const t3_problem *p, t3k::Call call, int need, const void *A
   // without; gemm_tile_kernel loses 6 % there with it, and gains 3 % where K or the output is large.)
   q.nt_out = (!two_writers &&
               (p->K >= kNtMinK || 4ll * p->M * p->N > kMemorySideCacheBytes)) ? 1 : 0;
-  q.timeline = g_timeline.load();
-  {
-    const int64_t wgs = g_timeline_wgs.load();
-    q.timeline_wgs = (int32_t)(wgs > (1ll << 30) ? (1ll << 30) : wgs);
-  }
+  set_timeline(q);
   q.wide = shape.kernel == t3k::kWideTile;
   if (q.wide) {
     q.order = t3k::tile_order(p, call, shape, t3k::xcd_rows(p, call, shape, blocks));
@@ -557,6 +559,7 @@ void plan_rounds(t3k::Plan &q, const t3k::Choice &c, const DeviceFacts &dev, int
   q.k_groups = dev.xcds > 1 ? dev.xcds : 0;
   q.by_groups = t3k::fast_div((uint32_t)(q.k_groups > 1 ? q.k_groups : 1));
   q.nt_out = bytes > kMemorySideCacheBytes ? 1 : 0;
+  set_timeline(q);
 }
 
 static_assert(T3_MAX_GROUPS == t3k::kMaxGroups, "groups of the header and of the kernels");
