@@ -34,7 +34,7 @@ UNITS = [("t3_api.hip", "t3_api.o", []), ("t3_i8_launch.hip", "t3_i8_launch.o", 
     for fn, mode, kn, km, overlap, i8 in [
         ("launch_wide_fused_i8", 1, 0, 0, 0, 1), ("launch_wide_overlap_i8", 1, 0, 0, 1, 1), ("launch_wide_gemm_i8", 0, 0, 0, 0, 1),
         ("launch_wide_grouped_nk", 2, 0, 0, 0, 0), ("launch_wide_grouped_kn", 2, 1, 0, 0, 0),
-        ("launch_wide_grouped_i8", 2, 0, 0, 0, 1), ("launch_wide_wgrad", 3, 1, 1, 0, 0)]]
+        ("launch_wide_grouped_i8", 2, 0, 0, 0, 1), ("launch_wide_wgrad", 3, 1, 1, 0, 0), ("launch_wide_wgrad_add", 4, 1, 1, 0, 0)]]
 DEPS = ["t3_api.hip", "t3_gemm_launch.hip", "t3_small_launch.hip", "t3_wide_launch.hip", "t3_choice.h", "t3_div.h", "t3_device.h", "t3_gemm.h",
         "t3_small.h", "t3_wide.h", "t3_aux.h", "t3_launch.h", "t3_i8_launch.hip", "t3_grouped_launch.hip", "t3_wide_products_launch.hip", "t3_groups.h", "t3_quant.h"]
 JOBS = 8

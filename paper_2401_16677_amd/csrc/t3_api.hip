@@ -827,7 +827,6 @@ t3_status t3_gemm_grouped_wgrad(const t3_grouped *g, const int32_t *offsets, con
   q.offsets = offsets;
   q.stride_b = g->stride_b;
   q.groups = g->groups;
-  q.accumulate = g->flags & T3_GROUPED_ACCUMULATE ? 1 : 0;
   DeviceFacts dev;
   st = device_facts(&dev);
   if (st != T3_OK) return st;
@@ -841,7 +840,9 @@ t3_status t3_gemm_grouped_wgrad(const t3_grouped *g, const int32_t *offsets, con
   q.by_tpc = t3k::fast_div((uint32_t)q.tpc);
   plan_rounds(q, c, dev, (int64_t)q.tpc * g->groups, 2ll * q.rows * (q.M + q.N) + 4ll * q.groups * q.M * q.N);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  return q.wide ? t3k::launch_wide_wgrad(q, tm, tn, s) : t3k::launch_small_wgrad(q, tm, tn, s);
+  const bool add = g->flags & T3_GROUPED_ACCUMULATE;
+  if (q.wide) return add ? t3k::launch_wide_wgrad_add(q, tm, tn, s) : t3k::launch_wide_wgrad(q, tm, tn, s);
+  return t3k::launch_small_wgrad(q, tm, tn, add, s);
 }
 
 t3_status t3_rs_reduce(const t3_problem *p, const float *C, float *R, void *fwd,

@@ -56,7 +56,8 @@ inline Choice workgroup_tile(const t3_problem *p, int cus, int64_t steps, bool w
   double best = -1.0;
   Choice pick{kSmallTile, kCand[5].t};
   for (const Cand &c : kCand) {
-    const bool general = c.stages && (!wide_ok || slabs < c.stages);
+    // (in 8 bits the wide-tile kernel has a slab of zeros for K of one slab, on the tiles of two stages)
+    const bool general = c.stages && (!wide_ok || (slabs < c.stages && !(i8 && c.stages == 2 && slabs == 1)));
     if (general && (c.t.n == 192 || i8)) continue;
     // (32 x 64 is for k-rows of B of a whole 128-byte line; with B K-contiguous two 32 x 32 workgroups take its place
     // at the same time per slab, and start and end sooner)
@@ -91,7 +92,7 @@ inline Choice grouped_tile(bool wgrad, bool kn, int64_t M, int64_t N, int64_t K,
     const double even = (double)M / c.t.m + 0.5 * used;
     const double T = (wgrad ? (double)(groups * ceil_div(M, c.t.m)) : (even > used ? even : used)) * columns, slots = (double)cus * c.per_cu;
     double slabs = wgrad ? (double)K / ((double)groups * 64.0) + 0.5 : (double)ceil_div(K, 64);
-    if (c.stages && (!wide_ok || (!wgrad && slabs < c.stages))) continue;
+    if (c.stages && (!wide_ok || (!wgrad && (c.stages == 2 ? K == 0 : slabs < c.stages)))) continue;
     if (slabs < c.stages) slabs = c.stages;
     const double rounds = T <= slots ? 1.0 : T / slots + 0.5, alone = c.per_cu == 2 && T <= cus ? 0.8 : 1.0;
     const double slab_us = c.slab_us * (wgrad && c.t.m == 32 ? 1.34 : 1.0) * ((wgrad || kn) && c.t.n == 32 ? 1.34 : 1.0);

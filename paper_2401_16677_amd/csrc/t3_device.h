@@ -30,7 +30,7 @@ constexpr uint32_t kFlagFwdDirect = 2u;
 constexpr uint32_t kFlagTwoWriters = 4u;
 constexpr uint32_t kFlagFwdBf16 = 8u;
 
-enum Mode { kModeGemm = 0, kModeFused = 1, kModeGrouped = 2, kModeWgrad = 3 };
+enum Mode { kModeGemm = 0, kModeFused = 1, kModeGrouped = 2, kModeWgrad = 3, kModeWgradAdd = 4 };
 
 // s_waitcnt immediates (gfx9 encoding: vmcnt[3:0] | expcnt << 4 | lgkmcnt << 8 | vmcnt[5:4] << 14)
 constexpr int kWaitVm0 = 0x0F70;
@@ -92,10 +92,11 @@ struct Plan {
   // scales of A's rows and of B's rows (of every group, one behind the other).
   const float *scale_a, *scale_b;
   // Products by group (t3_groups.h): `rows` rows sorted by group, group e's from offsets[e] on.  kModeGrouped: rows of A and C (M of
-  // them), group e times the operand at B + e stride_b.  kModeWgrad: A and B are both stored K x ..., K being a group's rows, the result is at R + e stride_b.
+  // them), group e times the operand at B + e stride_b.  kModeWgrad: A and B are both stored K x ..., K being a group's rows, the result is at R + e stride_b; kModeWgradAdd:
+  // it is added to what is there.
   const int32_t *offsets;
   int64_t stride_b;
-  int32_t groups, rows, accumulate;    // accumulate: results are added to what is there (kModeWgrad)
+  int32_t groups, rows;
 };
 
 struct Tile {

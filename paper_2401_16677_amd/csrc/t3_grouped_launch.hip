@@ -20,8 +20,8 @@ t3_status launch_small_grouped(const Plan &q, int32_t tm, int32_t tn, bool b_kn,
 t3_status launch_small_grouped_i8(const Plan &q, int32_t tm, int32_t tn, hipStream_t s) {
   return launch_small<kModeGrouped, 0, 0, 1>(q, tm, tn, s);
 }
-t3_status launch_small_wgrad(const Plan &q, int32_t tm, int32_t tn, hipStream_t s) {
-  return launch_small<kModeWgrad, 1, 1, 0>(q, tm, tn, s);
+t3_status launch_small_wgrad(const Plan &q, int32_t tm, int32_t tn, bool add, hipStream_t s) {
+  return add ? launch_small<kModeWgradAdd, 1, 1, 0>(q, tm, tn, s) : launch_small<kModeWgrad, 1, 1, 0>(q, tm, tn, s);
 }
 
 }  // namespace t3k

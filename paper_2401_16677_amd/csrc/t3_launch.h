@@ -61,10 +61,11 @@ t3_status launch_wide_gemm_i8(const Plan &q, int32_t tm, int32_t tn, hipStream_t
 // Products by group (t3_grouped_launch.hip).
 t3_status launch_small_grouped(const Plan &q, int32_t tm, int32_t tn, bool b_kn, hipStream_t s);
 t3_status launch_small_grouped_i8(const Plan &q, int32_t tm, int32_t tn, hipStream_t s);
-t3_status launch_small_wgrad(const Plan &q, int32_t tm, int32_t tn, hipStream_t s);
+t3_status launch_small_wgrad(const Plan &q, int32_t tm, int32_t tn, bool add, hipStream_t s);
 t3_status launch_wide_grouped_nk(const Plan &q, int32_t tm, int32_t tn, hipStream_t s);      // (t3_wide_products_launch.hip)
 t3_status launch_wide_grouped_kn(const Plan &q, int32_t tm, int32_t tn, hipStream_t s);
 t3_status launch_wide_grouped_i8(const Plan &q, int32_t tm, int32_t tn, hipStream_t s);
 t3_status launch_wide_wgrad(const Plan &q, int32_t tm, int32_t tn, hipStream_t s);
+t3_status launch_wide_wgrad_add(const Plan &q, int32_t tm, int32_t tn, hipStream_t s);
 
 }  // namespace t3k

@@ -23,7 +23,7 @@ namespace t3k {
 // take the place of finished ones find the lines in the scalar cache, and a request past it costs each of them 0.3 us (by scalar loads and
 // by vector: 24 x 12288 x 1536 on 8 chunks, 384 tiles of 32 x 32, 10.9 us, 10.8; 33 x 16000 x 256 on 2, 250 of 64 x 64,
 // 8.3, 8.1; 24 x 24576 x 1536 on 8, 768 of 32 x 32, 17.1, 17.7; 16 x 24576 x 4096 on 16 41.1, 42.4; 2097 x 1280 x 1472 on 32, 1056 of 64 x 64, 47.5, 48.1).
-// I8: operands in 8 bits, whose sums are integers up to where the incoming partial is added.  MODE kModeGrouped, kModeWgrad: products by
+// I8: operands in 8 bits, whose sums are integers up to where the incoming partial is added.  MODE kModeGrouped, kModeWgrad, kModeWgradAdd: products by
 // group, a tile being one group's.
 template <int BM, int BN, int WK, int NST, int MODE, int BKN, int AKM, bool WORDS, int I8 = 0>
 __global__ __launch_bounds__(64 * WK) void small_tile_kernel(const Plan arg) {
@@ -50,7 +50,7 @@ __global__ __launch_bounds__(64 * WK) void small_tile_kernel(const Plan arg) {
     if (MODE == kModeFused) gen = *(const __attribute__((address_space(4))) uint32_t *)(p.track + 2 * trk_bank_words(p.P));
   };
   if (WORDS) ask_generation();
-  constexpr bool grouped = MODE == kModeGrouped, wgrad = MODE == kModeWgrad;
+  constexpr bool grouped = MODE == kModeGrouped, wgrad = MODE >= kModeWgrad;
   Tile tl{0, 0, 0, 0};
   int row_lo = 0, row_hi = p.M;                  // rows of A and of the result the tile's are among
   if constexpr (grouped || wgrad) {
@@ -137,7 +137,7 @@ __global__ __launch_bounds__(64 * WK) void small_tile_kernel(const Plan arg) {
   // ---- this wavefront's rows of the tile: the incoming partial, behind the first slabs.  (The
   // waits for slabs below count the slabs' copies only: with these loads among them they wait for
   // a few copies more than they need, never fewer.)
-  const bool store_only = wgrad ? !p.accumulate : MODE != kModeFused || ((p.flags & kFlagStep0StoreOnly) && tl.s == 0);
+  const bool store_only = wgrad ? MODE == kModeWgrad : MODE != kModeFused || ((p.flags & kFlagStep0StoreOnly) && tl.s == 0);
   const bool direct = MODE == kModeFused && (p.flags & kFlagFwdDirect);
   const bool to_fwd = MODE == kModeFused && tl.c != p.own && (direct || chunk_is_whole(p, tl.s));
   const bool to_out = !direct || tl.c == p.own;

@@ -28,7 +28,7 @@
 // buffer: behind its last row, or kOob = 2^31 plus anything, with buffers of at most 2^31 bytes: the host sees to that.)
 //
 // The same kernel multiplies operands in 8 bits (I8: as many bytes a slab, 16 x 16 x 64 a product; the integer sums become floats times
-// their scales on the way out) and rows sorted by group (MODE kModeGrouped, kModeWgrad: see t3_groups.h; a piece of work is a tile of one group).
+// their scales on the way out) and rows sorted by group (MODE kModeGrouped, kModeWgrad, kModeWgradAdd: see t3_groups.h; a piece of work is a tile of one group).
 //
 // Included by the launch units only.
 #pragma once
@@ -125,7 +125,7 @@ __device__ __forceinline__ bool get_group_piece(PlanWords &words, const GroupRow
   w.rows = at.rows;
   if (MODE == kModeGrouped) {
     w.nf = p.K / kBK;
-    w.ns = w.nf + (p.K % kBK ? 1 : 0);
+    w.ns = max(w.nf + (p.K % kBK ? 1 : 0), 2);
   } else {
     w.nf = w.ns = max((at.rows + kBK - 1) / kBK, NSTAGE);
   }
@@ -145,7 +145,7 @@ void wide_tile_kernel(const Plan) {
   static_assert(PRE > 0 && PRE <= DEPTH && DEPTH <= FM && NL + PRE * FN < 64, "");
   __shared__ __attribute__((aligned(1024))) char lds[kImgOff + NIMG * kImgBytes];
 
-  constexpr bool tracked = MODE == kModeFused, grouped = MODE == kModeGrouped, wgrad = MODE == kModeWgrad;
+  constexpr bool tracked = MODE == kModeFused, grouped = MODE == kModeGrouped, wgrad = MODE >= kModeWgrad;
   const int lane = threadIdx.x & 63;
   PlanWords words;
   words.load(lane);
@@ -154,7 +154,11 @@ void wide_tile_kernel(const Plan) {
   if constexpr (grouped || wgrad) groups.load<BM>(p, lane);
   auto piece_of = [&](int it, Piece &w) {
     if constexpr (grouped || wgrad) return get_group_piece<MODE, BM, NSTAGE>(words, groups, it, w);
-    else return get_piece(words, it, w);
+    else {
+      const bool is = get_piece(words, it, w);
+      if constexpr (I8 && NSTAGE == 2) w.ns = max(w.ns, 2);                // (K of one slab)
+      return is;
+    }
   };
   // The tracker's generation, a scalar load nothing waits for until a tile is counted.  (Waited for here it puts a round trip
   // to memory in front of the first slabs.)  It is read as constant memory, which it is while this workgroup reads it: the launch's
@@ -166,6 +170,10 @@ void wide_tile_kernel(const Plan) {
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1;
   const int ktail = __builtin_amdgcn_readfirstlane(p.K % kBK);
+  // (8 bits, by group: K of one slab has a second one of zeros behind it, on the tiles of two stages: the first is the ragged one then, if
+  // there is one, and the second's buffers have no bytes)
+  constexpr bool kOneSlab = (I8 || grouped) && NSTAGE == 2;
+  const bool one_slab = kOneSlab && __builtin_amdgcn_readfirstlane(p.K) <= kBK;
   // bytes from one slab to the next in each operand
   const uint32_t a_step = __builtin_amdgcn_readfirstlane(AKM ? (uint32_t)p.lda * (kBK * 2) : (uint32_t)kRowBytes);
   const uint32_t b_step = __builtin_amdgcn_readfirstlane(BKN ? (uint32_t)p.ldb * (kBK * 2) : (uint32_t)kRowBytes);
@@ -313,6 +321,7 @@ void wide_tile_kernel(const Plan) {
     walkA = walk(a_step);
     if (AKM || BKN) walkB = walk(b_step);
   };
+  auto stream_end = [&]() { descA[2] = descB[2] = 0u; };          // (buffers of no bytes)
   auto stream_ragged = [&]() {                   // the stream's last slab ends with K: nothing behind it
     if constexpr (!AKM && !BKN) {
       walkA.at = walkA.end;
@@ -329,7 +338,14 @@ void wide_tile_kernel(const Plan) {
       markedA = true;
     }
   };
-  auto stream_end = [&]() { descA[2] = descB[2] = 0u; };          // (buffers of no bytes)
+  auto stream_piece = [&](const Piece &w) {
+    stream_to(w);
+    if (kOneSlab && one_slab && ktail) stream_ragged();
+  };
+  auto stream_last = [&]() {                     // on to the stream's last slab, if that is another kind than those before it
+    if (kOneSlab && one_slab) stream_end();
+    else stream_ragged();
+  };
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
   auto copy_one = [&](auto Q, uint32_t so) {     // of the slab the walks are at
@@ -462,11 +478,11 @@ void wide_tile_kernel(const Plan) {
   Piece cur;
   if (!piece_of(0, cur) && (grouped || wgrad)) return;             // (else the grid is no larger than the number of pieces)
   p = words.now();
-  stream_to(cur);
+  stream_piece(cur);
 #pragma unroll
   for (int j = 0; j < NSTAGE; ++j) {
     if (j) slab_next();
-    if (ktail && j == cur.ns - 1 && cur.ns > cur.nf) stream_ragged();
+    if ((ktail || (kOneSlab && one_slab)) && j == cur.ns - 1 && cur.ns > cur.nf) stream_last();
     static_for<NL>([&](auto Q) { copy_one(Q, (uint32_t)(j * kStageBytes)); });
   }
   asm volatile("s_waitcnt vmcnt(%0)" : : "n"((NSTAGE - 1) * NL) : "memory");      // slab 0 landed
@@ -488,7 +504,7 @@ void wide_tile_kernel(const Plan) {
     stamp(it, 0);
     const Tile tl = cur.tl;
     p = words.now();
-    const bool has_in = wgrad ? p.accumulate != 0 : cur.half == 2 || (tracked && !((p.flags & kFlagStep0StoreOnly) && tl.s == 0));
+    const bool has_in = wgrad ? MODE == kModeWgradAdd : cur.half == 2 || (tracked && !((p.flags & kFlagStep0StoreOnly) && tl.s == 0));
 
     if (cur.ns <= NSTAGE) flush();               // (too short a K loop to put the count off into)
     if (cur.half == 2 && wave == 0) {
@@ -646,7 +662,7 @@ void wide_tile_kernel(const Plan) {
       if (kt == k_switch) {
         more = piece_of(it + 1, nxt);
         p = words.now();
-        if (more) stream_to(nxt);
+        if (more) stream_piece(nxt);
         else stream_end();
         if (tracked && has_in) {
           p = words.now();
@@ -659,8 +675,8 @@ void wide_tile_kernel(const Plan) {
         }
       }
       // the slab copied next is the last one of the stream's piece, and ragged
-      if (ktail && (kt == k_switch - 1 || (kt == last && more && nxt.ns == NSTAGE)) && (kt < k_switch ? cur.ns > cur.nf : nxt.ns > nxt.nf))
-        stream_ragged();
+      if ((ktail || (kOneSlab && one_slab)) && (kt == k_switch - 1 || (kt == last && more && nxt.ns == NSTAGE)) && (kt < k_switch ? cur.ns > cur.nf : nxt.ns > nxt.nf))
+        stream_last();
       // the next barrier something is to be done behind, or whose wait is another one
       int stop = kt < k_switch ? (ktail && kt < k_switch - 1 ? k_switch - 1 : k_switch) : (NSTAGE > 2 && kt < last - 1 ? kt + 1 : last);
       if (kt < NSTAGE && (counting || (NSTAGE > 2 && it > 0))) stop = min(stop, kt + 1);
@@ -790,9 +806,8 @@ void wide_tile_kernel(const Plan) {
       } else {
         way_out(c0, true_type{});
       }
-    } else if (wgrad && has_in) {
-      if (nt_out) way_out(c0, true_type{});
-      else way_out(keep, true_type{});
+    } else if constexpr (MODE == kModeWgradAdd) {
+      way_out(c0, true_type{});                  // (one way out: with two the compiler waits for what is added where the next tile's products begin)
     } else if (!grouped && !wgrad && cur.half == 2) {
       way_out(keep, true_type{});
     } else {

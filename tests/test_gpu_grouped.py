@@ -95,6 +95,13 @@ def test_forward_large(N, K, counts):
     check_forward(counts, 0, 0, N, K, True, integers=True)
 
 
+@pytest.mark.parametrize("layout", ["nk", "kn"])
+@pytest.mark.parametrize("K", [8, 56, 64, 72, 128, 136])
+def test_forward_short_contraction(layout, K):
+    """K of one slab and of little more, in launches of several rounds."""
+    check_forward([700, 900, 1, 450, 0, 1300], 2, 3, 2560, K, layout == "kn", integers=K % 16 == 0)
+
+
 def test_no_contraction_and_no_rows():
     C = torch.full((6, 8), OUTSIDE, device=DEV)
     x = torch.zeros(512, dtype=torch.bfloat16, device=DEV)
@@ -150,7 +157,8 @@ def test_in_8_bits(case):
         assert bool((C[:first] == OUTSIDE).all()) and bool((C[o[-1]:] == OUTSIDE).all()) and bool((C[:, N:] == OUTSIDE).all())
 
 
-@pytest.mark.parametrize("N,K,counts", [(4096, 2048, [700, 300, 0, 1500]), (2048, 6144, [2, 0, 1, 5, 1, 1]), (2560, 1024, [2000, 1900])])
+@pytest.mark.parametrize("N,K,counts", [(4096, 2048, [700, 300, 0, 1500]), (2048, 6144, [2, 0, 1, 5, 1, 1]), (2560, 1024, [2000, 1900]),
+                                        (2560, 112, [900, 1, 0, 2500]), (2560, 128, [900, 1, 0, 2500]), (2560, 16, [900, 1, 0, 2500]), (2560, 144, [900, 3000])])
 def test_in_8_bits_large(N, K, counts):
     rows, E, g = sum(counts), len(counts), gen(3)
     A = torch.randint(-128, 128, (rows, K), generator=g, device=DEV, dtype=torch.int8)

@@ -77,7 +77,8 @@ def test_rows_that_are_no_numbers():
 # ------------------------------------------------------------------ the plain product
 
 SHAPES = [(1, 4, 16), (1, 1200, 1536), (3, 20, 48), (16, 516, 1040), (17, 100, 272), (33, 64, 64), (64, 260, 128), (100, 1000, 2000), (130, 772, 640),
-          (300, 1028, 1168), (515, 2052, 336), (1000, 600, 4112), (2048, 2560, 512), (257, 8200, 1536), (4100, 1540, 768)]
+          (300, 1028, 1168), (515, 2052, 336), (1000, 600, 4112), (2048, 2560, 512), (257, 8200, 1536), (4100, 1540, 768),
+          (2100, 2564, 112), (2100, 2564, 128), (3000, 5140, 16), (2100, 2564, 144)]
 
 
 @pytest.mark.parametrize("M,N,K", SHAPES)
@@ -130,7 +131,8 @@ def test_product_at_its_limits():
 FUSED = [(24, 1152, 1152, 16, 9, 0, (0, 0)), (100, 320, 400, 4, 3, t3.T3_FLAG_FWD_DIRECT, (128, 128)),
          (257, 1040, 640, 2, 0, t3.T3_FLAG_FWD_BF16 | t3.T3_FLAG_FWD_DIRECT, (0, 0)), (520, 2144, 336, 4, 1, t3.T3_FLAG_FWD_BF16, (256, 128)),
          (1000, 2128, 1072, 4, 2, t3.T3_FLAG_STEP0_STORE_ONLY, (128, 256)), (2040, 5120, 1040, 5, 2, t3.T3_FLAG_FWD_DIRECT, (256, 256)),
-         (1100, 3200, 576, 8, 7, t3.T3_FLAG_FWD_DIRECT | t3.T3_FLAG_STEP0_STORE_ONLY, (0, 0)), (700, 1504, 2000, 2, 1, 0, (0, 0)), (64, 64, 32, 1, 0, 0, (0, 0))]
+         (1100, 3200, 576, 8, 7, t3.T3_FLAG_FWD_DIRECT | t3.T3_FLAG_STEP0_STORE_ONLY, (0, 0)), (700, 1504, 2000, 2, 1, 0, (0, 0)), (64, 64, 32, 1, 0, 0, (0, 0)),
+         (2000, 4096, 112, 4, 1, t3.T3_FLAG_FWD_DIRECT, (256, 256)), (2300, 4256, 128, 8, 5, 0, (0, 0))]
 
 
 def fused_case(M, N, K, tp, seed=3):
