@@ -59,11 +59,12 @@ class T3Error(RuntimeError):
 
 
 _lib = None
+_float32 = None                                    # torch.float32, once torch is loaded
 
 
 def lib():
     """Load libt3.so (built in-tree by paper_2401_16677_amd.build).  Raises if it is missing."""
-    global _lib
+    global _lib, _float32
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise FileNotFoundError(
@@ -71,7 +72,8 @@ def lib():
         # The library must bind to the HIP runtime that owns the caller's device memory and
         # streams.  PyTorch ships its own copy, so it is loaded first and libt3.so's
         # dependency on libamdhip64 resolves to that one.
-        import torch  # noqa: F401
+        import torch
+        _float32 = torch.float32
         L = ctypes.CDLL(LIB_PATH)
         vp, i32, i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
         pp = ctypes.POINTER(T3Problem)
@@ -247,9 +249,10 @@ def t3_gemm(p, A, B, C, stream=None):
 
 
 def t3_quant_rows(rows, cols, x, q, scale, ldx=None, ldq=None, x_type=None, stream=None):
+    L = lib()
     if x_type is None:                             # a tensor's own type
-        x_type = T3_TYPE_F32 if str(getattr(x, "dtype", "")) == "torch.float32" else T3_TYPE_BF16
-    _check(lib().t3_quant_rows(rows, cols, x_type, _dptr(x), cols if ldx is None else ldx, _dptr(q),
+        x_type = T3_TYPE_F32 if getattr(x, "dtype", None) is _float32 else T3_TYPE_BF16
+    _check(L.t3_quant_rows(rows, cols, x_type, _dptr(x), cols if ldx is None else ldx, _dptr(q),
                                cols if ldq is None else ldq, _dptr(scale), _stream(stream)),
            "t3_quant_rows")
 

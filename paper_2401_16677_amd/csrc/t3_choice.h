@@ -67,6 +67,9 @@ inline Choice workgroup_tile(const t3_problem *p, int cus, int64_t steps, bool w
     const bool tail = c.stages && !general && c.per_cu == 1 && T > slots && T % slots && 2 * (T % slots) <= slots &&
                       p->K / 64 >= kTailMinSlabs && !(p->flags & T3_FLAG_FWD_BF16);
     if (tail) rounds -= 0.5;
+    // (8 bits: where small tiles of a second round take the places of the first one's as these end, two to a compute unit.  24 x 18432 x 1152 on 16 chunks, 576 of
+    // 32 x 32: 9.3 us, by 128 x 128 12.2; 51 x 19912 x 3952, 1246: 25.9, by 64 x 64 30.9.  bfloat16's rule is as it was)
+    if (i8 && c.t.m == 32 && T > slots) rounds = (double)T / (double)slots;
     // (a compute unit with one tile instead of two has it done in 0.8 of the time)
     const double alone = c.per_cu == 2 && T <= cus ? 0.8 : 1.0;
     // (k-rows of a transposed operand are half a 128-byte line long in a 32 wide tile)
@@ -94,8 +97,8 @@ inline Choice grouped_tile(bool wgrad, bool kn, int64_t M, int64_t N, int64_t K,
     double slabs = wgrad ? (double)K / ((double)groups * 64.0) + 0.5 : (double)ceil_div(K, 64);
     if (c.stages && (!wide_ok || (!wgrad && (c.stages == 2 ? K == 0 : slabs < c.stages)))) continue;
     if (slabs < c.stages) slabs = c.stages;
-    const double rounds = T <= slots ? 1.0 : T / slots + 0.5, alone = c.per_cu == 2 && T <= cus ? 0.8 : 1.0;
-    const double slab_us = c.slab_us * (wgrad && c.t.m == 32 ? 1.34 : 1.0) * ((wgrad || kn) && c.t.n == 32 ? 1.34 : 1.0);
+    const double rounds = T <= slots ? 1.0 : T / slots + (c.t.m == 32 ? 0.0 : 0.5), alone = c.per_cu == 2 && T <= cus ? 0.8 : 1.0;
+    const double slab_us = c.slab_us * (wgrad && c.t.m == 32 ? 1.34 : 1.0) * ((wgrad || kn) && c.t.n == 32 ? 1.7 : 1.0);
     const double us = rounds * alone * (c.ends_us + slab_us * slabs);
     if (best < 0 || us < best * 0.999) {
       best = us;

@@ -11,32 +11,36 @@ namespace t3k {
 constexpr int kQuantPieces = 8;        // pieces of 8 elements a lane holds at most
 
 // 127 x / a to the nearest integer, ties to even, as if the quotient were not rounded before: eight of them, in the bytes of two words.
-// inv = 127 / a, rounded.  x inv is off by less than 2^-15 (two roundings of half a step of numbers up to 127), and 1.5 2^23 + x inv has
-// the integer nearest to it in its low bits.  Where 2^-15 could decide, next to k + 1/2, the sign of 127 x - (k + 1/2) a does: 127 x in two
-// numbers p + rest, and p - (k + 1/2) a, a small multiple of a's last place or of x's, without a rounding.
-__device__ __forceinline__ u32x2 quantised(const float (&x)[8], float a, float inv) {
-  constexpr float kWhole = 12582912.0f, kNear = 0.5f - 0x1p-15f;
-  uint32_t n[8];
-  float off = 0.0f;
+// by_a = 1 / a, rounded.  127 x is a number p, of fp32 x with a rest; f = p by_a + (what p by_a misses, an exact remainder) by_a is the quotient with one
+// rounding but for 2^-46 of it, so it is on the quotient's side of every k + 1/2, or at k + 1/2 itself; 1.5 2^23 + f has the integer nearest to f in
+// its low bits.  Where f is k + 1/2 the remainder's sign decides.  (That is one number in 10^5, and behind a branch.)
+template <bool F32>
+__device__ __forceinline__ u32x2 quantised(const float (&x)[8], float a, float by_a) {
+  constexpr float kWhole = 12582912.0f;
+  float m[8], f[8], off = 0.0f;
+  auto remainder = [&](int e, float f) {
+    const float p = 127.0f * x[e], r = __builtin_fmaf(-f, a, p);
+    return F32 ? r + __builtin_fmaf(127.0f, x[e], -p) : r;
+  };
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float f = x[e] * inv, m = f + kWhole;
-    off = fmaxf(off, __builtin_fabsf(f - (m - kWhole)));
-    n[e] = __builtin_bit_cast(uint32_t, m);
+    const float f0 = 127.0f * x[e] * by_a;
+    f[e] = __builtin_fmaf(remainder(e, f0), by_a, f0);
+    m[e] = f[e] + kWhole;
+    off = fmaxf(off, __builtin_fabsf(f[e] - (m[e] - kWhole)));
   }
-  if (off > kNear) {
+  if (off == 0.5f) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float f = x[e] * inv, below = __builtin_floorf(f), at = f - below;
-      const float p = 127.0f * x[e], rest = __builtin_fmaf(127.0f, x[e], -p), past = __builtin_fmaf(-(below + 0.5f), a, p) + rest;
-      const int k = (int)below, up = past > 0.0f || (past == 0.0f && (k & 1)) ? k + 1 : k;
-      if (__builtin_fabsf(at - 0.5f) < 0x1p-14f) n[e] = (uint32_t)up;
+      const float d = f[e] - (m[e] - kWhole);
+      if (__builtin_fabsf(d) == 0.5f && remainder(e, f[e]) * d > 0.0f) m[e] += 2.0f * d;
     }
   }
-  auto four = [](uint32_t b0, uint32_t b1, uint32_t b2, uint32_t b3) {        // low bytes together
-    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(b3, b2, 0x0c0c0400u), __builtin_amdgcn_perm(b1, b0, 0x0c0c0400u), 0x05040100u);
+  auto four = [&](int e) {                       // low bytes together
+    auto b = [&](int i) { return __builtin_bit_cast(uint32_t, m[e + i]); };
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(b(3), b(2), 0x0c0c0400u), __builtin_amdgcn_perm(b(1), b(0), 0x0c0c0400u), 0x05040100u);
   };
-  return u32x2{four(n[0], n[1], n[2], n[3]), four(n[4], n[5], n[6], n[7])};
+  return u32x2{four(0), four(4)};
 }
 
 // PIECES: of 8 elements that a lane holds at a time.
@@ -90,20 +94,22 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const void *x, int64_t 
   const bool finite = top < 0x7F800000u, any = top != 0u && finite;
   const float largest = __builtin_bit_cast(float, top);
   if (lane == 0) scale[row] = finite ? __fdiv_rn(largest, 127.0f) : __builtin_nanf("");
-  // (rows whose 127 / a or 127 x might not be a float are taken at another power of two, which changes no quotient; elements that would fall
-  // below the smallest float are nowhere near 1/2)
-  const float by = largest < 0x1p-60f ? 0x1p100f : (largest > 0x1p100f ? 0x1p-20f : 1.0f), a = largest * by, inv = __fdiv_rn(127.0f, a);
+  // (rows whose 1 / a or 127 x might not be a float, or whose remainders might be too small for one, are taken at another power of two, which
+  // changes no quotient; elements that would fall below the smallest float are nowhere near 1/2)
+  const float by = largest < 0x1p-40f ? 0x1p100f : (largest > 0x1p100f ? 0x1p-20f : 1.0f), a = largest * by, by_a = __fdiv_rn(1.0f, a);
   int8_t *to = q + row * ldq;
   for (int base = 0; base == 0 || base < pieces; base += kHeld) {
     if (pieces > kHeld) load(base);
+    if (by != 1.0f) {
+#pragma unroll
+      for (int u = 0; u < PIECES; ++u)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[u][e] *= by;
+    }
 #pragma unroll
     for (int u = 0; u < PIECES; ++u) {
       const int at = base + u * TEAM + lane;
-      if (by != 1.0f) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[u][e] *= by;
-      }
-      if (at < pieces) ((u32x2 *)to)[at] = any ? quantised(v[u], a, inv) : u32x2{0, 0};
+      if (at < pieces) ((u32x2 *)to)[at] = any ? quantised<F32>(v[u], a, by_a) : u32x2{0, 0};
     }
   }
 }
