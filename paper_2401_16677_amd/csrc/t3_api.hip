@@ -553,6 +553,7 @@ void plan_rounds(t3k::Plan &q, const t3k::Choice &c, const DeviceFacts &dev, int
   q.wide = c.kernel == t3k::kWideTile;
   q.Wt = (int32_t)ceil_div(q.N, c.tile.n);
   q.resident = dev.cus * (c.tile.m == 128 && c.tile.n == 128 ? 2 : 1);
+  q.cut = t3k::quarters_of(c.tile) && most_tiles > q.resident ? t3k::kCutLeave : t3k::kCutNone;
   q.order.round = (uint32_t)q.resident;
   q.order.by_round = t3k::fast_div(q.order.round);
   q.total_blocks = (int32_t)((most_tiles + 7) / 8 * 8);
@@ -560,6 +561,15 @@ void plan_rounds(t3k::Plan &q, const t3k::Choice &c, const DeviceFacts &dev, int
   q.by_groups = t3k::fast_div((uint32_t)(q.k_groups > 1 ? q.k_groups : 1));
   q.nt_out = bytes > kMemorySideCacheBytes ? 1 : 0;
   set_timeline(q);
+}
+
+// The launch, and behind it the one of a last round's tiles in quarters (which has nothing to do if that round is fuller, or if there is none).
+t3_status launch_rounds(t3k::Plan &q, t3_status (*launch_fn)(const t3k::Plan &, int32_t, int32_t, hipStream_t), hipStream_t s) {
+  const t3_status st = launch_fn(q, q.tile_m, q.tile_n, s);
+  if (st != T3_OK || q.cut != t3k::kCutLeave) return st;
+  q.cut = t3k::kCutQuarters;
+  q.total_blocks = q.resident *= 2;              // (two workgroups of 128 x 128 to a compute unit)
+  return launch_fn(q, 128, 128, s);
 }
 
 static_assert(T3_MAX_GROUPS == t3k::kMaxGroups, "groups of the header and of the kernels");
@@ -601,8 +611,7 @@ t3_status grouped_product(const t3_grouped *g, bool i8, const int32_t *offsets, 
   plan_rounds(q, c, dev, (ceil_div(g->rows, tm) + (g->rows < g->groups ? g->rows : g->groups)) * ceil_div(g->N, tn),
               2ll * q.rows * q.K + 2ll * q.groups * q.N * q.K + 4ll * q.rows * q.N);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (q.wide)
-    return i8 ? t3k::launch_wide_grouped_i8(q, tm, tn, s) : (kn ? t3k::launch_wide_grouped_kn(q, tm, tn, s) : t3k::launch_wide_grouped_nk(q, tm, tn, s));
+  if (q.wide) return launch_rounds(q, i8 ? t3k::launch_wide_grouped_i8 : (kn ? t3k::launch_wide_grouped_kn : t3k::launch_wide_grouped_nk), s);
   return i8 ? t3k::launch_small_grouped_i8(q, tm, tn, s) : t3k::launch_small_grouped(q, tm, tn, kn, s);
 }
 
@@ -841,7 +850,7 @@ t3_status t3_gemm_grouped_wgrad(const t3_grouped *g, const int32_t *offsets, con
   plan_rounds(q, c, dev, (int64_t)q.tpc * g->groups, 2ll * q.rows * (q.M + q.N) + 4ll * q.groups * q.M * q.N);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bool add = g->flags & T3_GROUPED_ACCUMULATE;
-  if (q.wide) return add ? t3k::launch_wide_wgrad_add(q, tm, tn, s) : t3k::launch_wide_wgrad(q, tm, tn, s);
+  if (q.wide) return launch_rounds(q, add ? t3k::launch_wide_wgrad_add : t3k::launch_wide_wgrad, s);
   return t3k::launch_small_wgrad(q, tm, tn, add, s);
 }
 

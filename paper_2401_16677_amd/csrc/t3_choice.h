@@ -4,6 +4,8 @@
 
 #include <stdint.h>
 
+#include <cmath>
+
 #include "t3.h"
 #include "t3_div.h"
 
@@ -83,13 +85,23 @@ inline Choice workgroup_tile(const t3_problem *p, int cus, int64_t steps, bool w
   return pick;
 }
 
+// Products by group: tiles of which a last round of at most half the workgroups is done in quarters, by a second launch.
+inline bool quarters_of(TileShape t) { return t.m >= 192 && t.n == 256; }
+// Rounds that x rounds of tiles take: the last one whole, or as quarters 0.55.
+inline double rounds_of(double x, bool quarters) {
+  const double whole = (double)(int64_t)x, rest = x - whole;
+  if (rest <= 0.0) return whole;
+  return whole + (quarters && whole >= 1.0 && rest <= 0.5 ? 0.55 : 1.0);
+}
 // The tile of products by group, by the same times.  The host knows the rows of all groups together, so the tiles are those of groups
-// as large as the average, every one with half a tile more than its rows fill (or one tile), and the rounds those of tiles that fill the
-// last one half.  M x N: C, or the gradient of a group's weights (wgrad), whose K is a group's rows.
+// as large as the average, every one with half a tile more than its rows fill (or one tile), give or take what groups' ends make of it.  M x N: C, or the
+// gradient of a group's weights (wgrad), whose K is a group's rows.
 inline Choice grouped_tile(bool wgrad, bool kn, int64_t M, int64_t N, int64_t K, int64_t groups, int cus, bool wide_ok) {
   double best = -1.0;
   Choice pick{kSmallTile, {64, 64}};
-  for (const Cand &c : kCand) {
+  constexpr Cand kTall{{192, 256}, 2, 1, 0.92, 13.3};
+  for (int i = -1; i < (int)(sizeof(kCand) / sizeof(kCand[0])); ++i) {
+    const Cand &c = i < 0 ? kTall : kCand[i];
     if (c.t.m == 32 && c.t.n == 64) continue;
     const double used = (double)(wgrad || M > groups ? groups : M), columns = (double)ceil_div(N, c.t.n);
     const double even = (double)M / c.t.m + 0.5 * used;
@@ -97,7 +109,12 @@ inline Choice grouped_tile(bool wgrad, bool kn, int64_t M, int64_t N, int64_t K,
     double slabs = wgrad ? (double)K / ((double)groups * 64.0) + 0.5 : (double)ceil_div(K, 64);
     if (c.stages && (!wide_ok || (!wgrad && (c.stages == 2 ? K == 0 : slabs < c.stages)))) continue;
     if (slabs < c.stages) slabs = c.stages;
-    const double rounds = T <= slots ? 1.0 : T / slots + (c.t.m == 32 ? 0.0 : 0.5), alone = c.per_cu == 2 && T <= cus ? 0.8 : 1.0;
+    // (the ends of `used` groups, each anywhere in a tile: a standard deviation of 0.29 tiles of rows each)
+    const double off = !wgrad && even > used ? 0.5 * std::sqrt(used) * columns / slots : 0.0, x = T / slots;
+    double rounds = 0.0;
+    for (int k = -4; k <= 4; ++k) rounds += rounds_of(x + off * k / 4.0 > 0.0 ? x + off * k / 4.0 : x, quarters_of(c.t)) / 9.0;
+    if (c.t.m == 32) rounds = x > 1.0 ? x : 1.0;
+    const double alone = c.per_cu == 2 && T <= cus ? 0.8 : 1.0;
     const double slab_us = c.slab_us * (wgrad && c.t.m == 32 ? 1.34 : 1.0) * ((wgrad || kn) && c.t.n == 32 ? 1.7 : 1.0);
     const double us = rounds * alone * (c.ends_us + slab_us * slabs);
     if (best < 0 || us < best * 0.999) {

@@ -32,6 +32,8 @@ constexpr uint32_t kFlagFwdBf16 = 8u;
 
 enum Mode { kModeGemm = 0, kModeFused = 1, kModeGrouped = 2, kModeWgrad = 3, kModeWgradAdd = 4 };
 
+enum Cut { kCutNone = 0, kCutLeave = 1, kCutQuarters = 2 };
+
 // s_waitcnt immediates (gfx9 encoding: vmcnt[3:0] | expcnt << 4 | lgkmcnt << 8 | vmcnt[5:4] << 14)
 constexpr int kWaitVm0 = 0x0F70;
 constexpr int kWaitLgkm0 = 0xF0FF;    // and-mask that turns a wait into "... and lgkmcnt(0)"
@@ -96,7 +98,9 @@ struct Plan {
   // it is added to what is there.
   const int32_t *offsets;
   int64_t stride_b;
-  int32_t groups, rows;
+  // cut: tiles of a last round that would occupy at most half the workgroups are left (kCutLeave) to a second launch, which does them in
+  // quarters (kCutQuarters; tile_m x tile_n, Wt, Mt and order.round are those of the first).
+  int32_t groups, rows, cut;
 };
 
 struct Tile {

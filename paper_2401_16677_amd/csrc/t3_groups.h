@@ -17,7 +17,7 @@ constexpr int kMaxGroups = 256;
 
 struct GroupTile {
   int group, row0, rows;               // the group, its first row, how many it has
-  int mi, nj;                          // row and column of the tile in the group
+  int mi, nj;                          // row and column of the tile in the group (of the result, if its rows are not the group's)
 };
 
 template <int CTRL, int ROWS>
@@ -40,8 +40,8 @@ struct GroupRows {
   uint32_t end[kSets], tiles[kSets];   // lane l of set r, group 64 r + l: behind its last row; rows of tiles up to and with it
   uint32_t first, all_tiles;           // first row of the first group; rows of tiles of all groups
 
-  template <int BM>
-  __device__ __forceinline__ void load(const Plan &p, int lane) {
+  // bm: rows of a tile
+  __device__ __forceinline__ void load(const Plan &p, int lane, uint32_t bm) {
     const __amdgpu_buffer_rsrc_t r = make_rsrc(p.offsets, (uint32_t)(p.groups + 1) * 4u);
     auto offset = [&](int i) {                   // (past the array's end 0: no rows)
       return (uint32_t)min(max((int)__builtin_amdgcn_raw_buffer_load_b32(r, i * 4, 0, 0), 0), p.rows);
@@ -59,7 +59,7 @@ struct GroupRows {
       if (s == 0 || p.groups > 64 * s) {
         const uint32_t e = lane_scan(max(v[s], before), [](uint32_t a, uint32_t b) { return max(a, b); });
         const uint32_t rows = e - dpp<0x138, 0xf>(before, e);               // (the lane before's; lane 0: the set before's last)
-        const uint32_t t = lane_scan((rows + BM - 1) / BM, [](uint32_t a, uint32_t b) { return a + b; }) + count;
+        const uint32_t t = lane_scan((rows + bm - 1) / bm, [](uint32_t a, uint32_t b) { return a + b; }) + count;
         end[s] = e;
         tiles[s] = t;
         before = __builtin_amdgcn_readlane(e, 63);
@@ -95,26 +95,40 @@ struct GroupRows {
     t.mi = (int)row;
     t.nj = (int)(4u * band + in - row * width);
   }
-  // Tile at grid position b of products whose rows are grouped
-  __device__ __forceinline__ bool tile_at(const Plan &p, uint32_t b, GroupTile &t) const {
+  // Tiles of products whose rows are grouped, and of products whose contraction runs over a group's rows (tpc for every group)
+  template <bool ROWS>
+  __device__ __forceinline__ uint32_t count(const Plan &p) const { return ROWS ? all_tiles * (uint32_t)p.Wt : (uint32_t)p.groups * (uint32_t)p.tpc; }
+  // How many of n tiles the first launch does where the last round's may be cut: the others are at most half a round.
+  __device__ __forceinline__ static uint32_t uncut(const Plan &p, uint32_t n) {
+    const uint32_t round = p.order.round, left = n - div_by(n, p.order.by_round) * round;
+    return n > round && 2u * left <= round ? n - left : n;
+  }
+  template <bool ROWS>
+  __device__ __forceinline__ void tile(const Plan &p, uint32_t at, GroupTile &t) const {
+    if (ROWS) tile_at(p, at, t);
+    else tile_of_all(p, at, t);
+  }
+  // The tile at grid position b; false: behind the last one.
+  template <bool ROWS>
+  __device__ __forceinline__ bool tile_of_position(const Plan &p, uint32_t b, GroupTile &t) const {
+    const uint32_t n = count<ROWS>(p);
     uint32_t at;
-    if (!place(p, b, all_tiles * (uint32_t)p.Wt, at)) return false;
+    if (!place(p, b, p.cut == kCutLeave ? uncut(p, n) : n, at)) return false;
+    tile<ROWS>(p, at, t);
+    return true;
+  }
+  __device__ __forceinline__ void tile_at(const Plan &p, uint32_t at, GroupTile &t) const {
     int g = 0;
 #pragma unroll
     for (int s = 0; s < kSets; ++s) g += __builtin_popcountll(__ballot(tiles[s] * (uint32_t)p.Wt <= at));
     rows_of(g, t);
     const uint32_t before = g ? of(tiles, g - 1) : 0u, Mt = of(tiles, g) - before, q = at - before * (uint32_t)p.Wt;
     in_group(q, Mt, (uint32_t)p.Wt, t);
-    return true;
   }
-  // ... and of products whose contraction runs over a group's rows: tpc tiles for every group.
-  __device__ __forceinline__ bool tile_of_all(const Plan &p, uint32_t b, GroupTile &t) const {
-    uint32_t at;
-    if (!place(p, b, (uint32_t)p.groups * (uint32_t)p.tpc, at)) return false;
+  __device__ __forceinline__ void tile_of_all(const Plan &p, uint32_t at, GroupTile &t) const {
     const uint32_t g = div_by(at, p.by_tpc);
     rows_of((int)g, t);
     in_group(at - g * (uint32_t)p.tpc, (uint32_t)p.Mt, (uint32_t)p.Wt, t);
-    return true;
   }
 };
 

@@ -55,9 +55,9 @@ __global__ __launch_bounds__(64 * WK) void small_tile_kernel(const Plan arg) {
   int row_lo = 0, row_hi = p.M;                  // rows of A and of the result the tile's are among
   if constexpr (grouped || wgrad) {
     GroupRows g;
-    g.load<BM>(p, lane);
+    g.load(p, lane, BM);
     GroupTile at;
-    if (grouped ? !g.tile_at(p, blockIdx.x, at) : !g.tile_of_all(p, blockIdx.x, at)) return;
+    if (!g.tile_of_position<grouped>(p, blockIdx.x, at)) return;
     tl = Tile{0, 0, at.mi, at.nj};
     if (grouped) {
       row_lo = at.row0;

@@ -85,7 +85,8 @@ struct Piece {
   Tile tl;
   int k0, nf, ns;      // first K-slab, full slabs, slabs with a ragged last one
   int half, idx;       // 0: whole tile, 1 / 2: first / second half of split tile idx
-  int row0, rows;      // products by group: the rows of the tile's group (tl.s), tl.c being 0
+  // products by group: the rows of the tile's group (tl.s; tl.c is 0), and the tile's own among the result's
+  int row0, rows, m0, m_rows;
 };
 // (each part of it reads of the plan what it needs: what is read is read, and kept, whether the branch is taken or not)
 __device__ __forceinline__ bool get_piece(PlanWords &words, int it, Piece &w) {
@@ -113,13 +114,36 @@ __device__ __forceinline__ bool get_piece(PlanWords &words, int it, Piece &w) {
 }
 
 // Products by group.  (As many slabs as there are stages at least: behind a group's rows they are zeros.)
-template <int MODE, int BM, int NSTAGE>
-__device__ __forceinline__ bool get_group_piece(PlanWords &words, const GroupRows &groups, int it, Piece &w) {
+// pos: this workgroup's next grid position.  CUT: quarters of tiles of 256 columns and at most 256 rows (see kCutQuarters).
+template <int MODE, int BM, int BN, int NSTAGE, int CUT>
+__device__ __forceinline__ bool get_group_piece(PlanWords &words, const GroupRows &groups, uint32_t &pos, Piece &w) {
   const Plan p = words.now();
+  constexpr bool kRows = MODE == kModeGrouped;
   GroupTile at;
-  const uint32_t pos = blockIdx.x + (uint32_t)it * (uint32_t)p.resident;
-  if (MODE == kModeGrouped ? !groups.tile_at(p, pos, at) : !groups.tile_of_all(p, pos, at)) return false;
-  w.tl = Tile{at.group, 0, at.mi, at.nj};
+  for (;;) {
+    if constexpr (CUT) {
+      const uint32_t n = groups.count<kRows>(p), first = groups.uncut(p, n), quarters = 4u * (n - first);
+      uint32_t q = pos;                          // (there are at most as many quarters as places: half a round of tiles, two places to a compute unit)
+      pos += (uint32_t)p.resident;
+      if (q >= quarters) return false;
+      q = (quarters >> 3) * (q & 7) + min(quarters & 7, q & 7) + (q >> 3);           // (an XCD's in a run)
+      groups.tile<kRows>(p, first + (q >> 2), at);
+      w.tl = Tile{at.group, 0, 0, 2 * at.nj + (int)(q >> 1 & 1)};
+      const int begin = at.mi * p.tile_m, end = min(begin + p.tile_m, kRows ? at.rows : p.M);
+      w.m0 = begin + (int)(q & 1) * BM;
+      w.m_rows = min(BM, end - w.m0);
+      if (w.m_rows <= 0 || w.tl.nj * BN >= p.W) continue;
+    } else {
+      const uint32_t q = pos;
+      pos += (uint32_t)p.resident;
+      if (!groups.tile_of_position<kRows>(p, q, at)) return false;
+      w.tl = Tile{at.group, 0, at.mi, at.nj};
+      w.m0 = at.mi * BM;
+      w.m_rows = min(BM, (kRows ? at.rows : p.M) - w.m0);
+    }
+    break;
+  }
+  if (kRows) w.m0 += at.row0;
   w.k0 = w.half = w.idx = 0;
   w.row0 = at.row0;
   w.rows = at.rows;
@@ -132,7 +156,7 @@ __device__ __forceinline__ bool get_group_piece(PlanWords &words, const GroupRow
   return true;
 }
 
-template <int FM, int FN, int NSTAGE, int NIMG, int PRE, int DEPTH, int MODE, int BKN, int AKM, int OVERLAP, int I8 = 0>
+template <int FM, int FN, int NSTAGE, int NIMG, int PRE, int DEPTH, int MODE, int BKN, int AKM, int OVERLAP, int I8 = 0, int CUT = 0>
 __global__ __launch_bounds__(256)
 __attribute__((amdgpu_waves_per_eu((32 * (FM + FN) * 128 * NSTAGE + NIMG * 4096 * FN) <= 80 * 1024 ? 2 : 1)))
 void wide_tile_kernel(const Plan) {
@@ -151,9 +175,10 @@ void wide_tile_kernel(const Plan) {
   words.load(lane);
   Plan p = words.now();                          // (read anew where something rare begins)
   GroupRows groups;
-  if constexpr (grouped || wgrad) groups.load<BM>(p, lane);
+  if constexpr (grouped || wgrad) groups.load(p, lane, CUT ? (uint32_t)p.tile_m : (uint32_t)BM);
+  uint32_t next_pos = blockIdx.x;
   auto piece_of = [&](int it, Piece &w) {
-    if constexpr (grouped || wgrad) return get_group_piece<MODE, BM, NSTAGE>(words, groups, it, w);
+    if constexpr (grouped || wgrad) return get_group_piece<MODE, BM, BN, NSTAGE, CUT>(words, groups, next_pos, w);
     else {
       const bool is = get_piece(words, it, w);
       if constexpr (I8 && NSTAGE == 2) w.ns = max(w.ns, 2);                // (K of one slab)
@@ -278,8 +303,8 @@ void wide_tile_kernel(const Plan) {
   };
   Walk walkA, walkB;
   auto stream_to = [&](const Piece &w) {
-    const int m0 = (grouped ? w.row0 : 0) + w.tl.mi * BM, at = col_at(w.tl), n0 = w.tl.c * p.W + at;
-    const int rows = min(BM, (grouped ? w.row0 + w.rows : p.M) - m0), cols = cols_of(w.tl, at);
+    const int m0 = grouped || wgrad ? w.m0 : w.tl.mi * BM, at = col_at(w.tl), n0 = w.tl.c * p.W + at;
+    const int rows = grouped || wgrad ? w.m_rows : min(BM, p.M - m0), cols = cols_of(w.tl, at);
     // (arrays of less than 2^31 elements: offsets in them are 32-bit products)
     const uint32_t lda = (uint32_t)p.lda, ldb = (uint32_t)p.ldb;
     if constexpr (grouped) p.B += w.tl.s * p.stride_b;
@@ -547,8 +572,8 @@ void wide_tile_kernel(const Plan) {
     };
     auto place = [&]() {
       Place o;
-      const int m0 = (grouped ? cur.row0 : 0) + tl.mi * BM, at = col_at(tl), n0 = tl.c * p.W + at;
-      o.rows_in = (uint32_t)min(BM, (grouped ? cur.row0 + cur.rows : p.M) - m0);
+      const int m0 = grouped || wgrad ? cur.m0 : tl.mi * BM, at = col_at(tl), n0 = tl.c * p.W + at;
+      o.rows_in = (uint32_t)(grouped || wgrad ? cur.m_rows : min(BM, p.M - m0));
       o.cols_in = cols_of(tl, at);
       if constexpr (wgrad) p.R += tl.s * p.stride_b;
       const bool direct = (p.flags & kFlagFwdDirect) != 0;
@@ -606,7 +631,7 @@ void wide_tile_kernel(const Plan) {
     float scale_a[FM];
     f32x4 scale_b[UB];
     auto load_scales = [&]() {
-      const int m0 = (grouped ? cur.row0 : 0) + tl.mi * BM, n0 = tl.c * p.W + col_at(tl);
+      const int m0 = grouped ? cur.m0 : tl.mi * BM, n0 = tl.c * p.W + col_at(tl);
       const float *of_rows = p.scale_a + m0, *of_columns = p.scale_b + ((grouped ? (int64_t)tl.s * p.N : 0) + n0);
       const __amdgpu_buffer_rsrc_t a_rsrc = make_rsrc(of_rows, (uint32_t)(p.M - m0) * 4u), b_rsrc = make_rsrc(of_columns, (uint32_t)(p.N - n0) * 4u);
       static_for<FM>([&](auto I) {

@@ -45,3 +45,34 @@ def close(got, want, bound):
     assert torch.equal(got.isnan(), nan)
     far = ((got - want).abs() - bound).masked_fill(nan, -1.0)
     assert far.numel() == 0 or float(far.max()) <= 0.0, (float(far.max()), int((far > 0).sum()), [int(i) for i in (far > 0).nonzero()[0]])
+
+
+_choice = None
+
+
+def grouped_tile(wgrad, kn, M, N, K, groups, cus=256, wide_ok=True):
+    """(wide-tile kernel, tile rows, tile columns, a last round may be cut in quarters) of a product by group, K in 2-byte elements."""
+    global _choice
+    if _choice is None:
+        import ctypes
+        import os
+        import subprocess
+        import tempfile
+        here = os.path.dirname(os.path.abspath(__file__))
+        root = os.path.dirname(here)
+        with tempfile.TemporaryDirectory() as d:
+            so = os.path.join(d, "grouped_choice.so")
+            subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-I", os.path.join(root, "include"), "-I",
+                            os.path.join(root, "paper_2401_16677_amd", "csrc"), os.path.join(here, "grouped_choice.cpp"), "-o", so], check=True)
+            _choice = ctypes.CDLL(so)
+        _choice.grouped_tile.argtypes = [ctypes.c_int] * 2 + [ctypes.c_int64] * 4 + [ctypes.c_int] * 2 + [ctypes.c_void_p]
+    import ctypes
+    out = (ctypes.c_int32 * 4)()
+    _choice.grouped_tile(int(wgrad), int(kn), M, N, K, groups, cus, int(wide_ok), ctypes.cast(out, ctypes.c_void_p))
+    return bool(out[0]), out[1], out[2], bool(out[3])
+
+
+def quarters(counts, N, tile, places=256):
+    """(tiles of the groups, those of the last round that are done in quarters)"""
+    T = sum(-(-n // tile[0]) for n in counts) * -(-N // tile[1])
+    return T, T % places if T > places and 2 * (T % places) <= places else 0

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2401_16677_amd import binding as t3
-from products import HALF, MORE, close, product8, rows8, spans
+from products import HALF, MORE, close, grouped_tile, product8, quarters, rows8, spans
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -100,6 +100,52 @@ def test_forward_large(N, K, counts):
 def test_forward_short_contraction(layout, K):
     """K of one slab and of little more, in launches of several rounds."""
     check_forward([700, 900, 1, 450, 0, 1300], 2, 3, 2560, K, layout == "kn", integers=K % 16 == 0)
+
+
+# rows of every group, and how many tiles of the last round are done in quarters (0: a full round, or one more than half full)
+ROUNDS = [([3000, 2000, 500, 500], 64), ([1400, 1400, 1600, 1600], 112), ([0, 2900, 1, 1600, 1000, 500], 112), ([1600, 1600, 1800, 1300], 0), ([4096, 4096], 0)]
+
+
+@pytest.mark.parametrize("layout", ["nk", "kn", "8 bits"])
+@pytest.mark.parametrize("counts,cut", ROUNDS)
+@pytest.mark.parametrize("N", [6144, 6104])
+def test_last_round_in_quarters(counts, cut, N, layout):
+    K, rows, E, kn = 1024, sum(counts), len(counts), layout == "kn"
+    choice = grouped_tile(False, kn, rows + 3, N, K, E)
+    assert choice == (True, 256, 256, True) and quarters(counts, N, (256, 256))[1] == cut
+    if layout == "8 bits":
+        g, o = gen(cut + N), offsets_of(counts, 1)
+        A = torch.randint(-128, 128, (rows + 3, 2 * K), generator=g, device=DEV, dtype=torch.int8)
+        B = torch.randint(-128, 128, (E, N, 2 * K), generator=g, device=DEV, dtype=torch.int8)
+        sa, sb = torch.exp(torch.randn(rows + 3, generator=g, device=DEV)), torch.exp(torch.randn((E, N), generator=g, device=DEV))
+        C = torch.full((rows + 3, N), OUTSIDE, device=DEV)
+        t3.t3_gemm_grouped_i8(t3.grouped(rows + 3, E, N, 2 * K), device(o), A, sa, B, sb, C)
+        for e, (a, b) in enumerate(spans(o, rows + 3)):
+            close(C[a:b], *product8(A[a:b], sa[a:b], B[e], sb[e]))
+        assert bool((C[:1] == OUTSIDE).all()) and bool((C[o[-1]:] == OUTSIDE).all())
+    else:
+        check_forward(counts, 1, 2, N, K, kn, integers=N % 256 == 0)
+
+
+@pytest.mark.parametrize("layout", ["nk", "kn"])
+def test_tiles_of_192_rows(layout):
+    counts = [183, 265, 302, 304, 311, 351, 356, 359, 404, 489, 541, 674, 750, 793, 953, 1155]
+    N, K, kn = (1280, 2560, True) if layout == "kn" else (5120, 1280, False)
+    assert grouped_tile(False, kn, sum(counts), N, K, 16) == (True, 192, 256, True)
+    check_forward(counts, 0, 0, N, K, kn)
+    check_forward(counts[::-1], 0, 0, N - 8, K, kn, integers=True)
+
+
+@pytest.mark.parametrize("layout", ["nk", "kn"])
+@pytest.mark.parametrize("add", [False, True])
+def test_wgrad_last_round_in_quarters(layout, add):
+    counts = [183, 265, 0, 606, 311, 351, 356, 359, 404, 489, 541, 674, 750, 793, 953, 1155]
+    for N, K in [(5120, 1280), (5112, 1272)]:
+        M, n = (K, N) if layout == "kn" else (N, K)
+        choice = grouped_tile(True, True, M, n, sum(counts), 16)
+        T = 16 * -(-M // choice[1]) * -(-n // choice[2])
+        assert choice[3] and 0 < T % 256 <= 128
+        check_wgrad(counts, 0, 0, N, K, layout == "kn", add, N == 5120)
 
 
 def test_no_contraction_and_no_rows():
