@@ -503,11 +503,16 @@ void wide_tile_kernel(const Plan) {
   Piece cur;
   if (!piece_of(0, cur) && (grouped || wgrad)) return;             // (else the grid is no larger than the number of pieces)
   p = words.now();
-  stream_piece(cur);
+  if constexpr (kOneSlab) stream_piece(cur);     // (as it was for the others: their code depends on how calls are nested)
+  else stream_to(cur);
 #pragma unroll
   for (int j = 0; j < NSTAGE; ++j) {
     if (j) slab_next();
-    if ((ktail || (kOneSlab && one_slab)) && j == cur.ns - 1 && cur.ns > cur.nf) stream_last();
+    if constexpr (kOneSlab) {
+      if ((ktail || one_slab) && j == cur.ns - 1 && cur.ns > cur.nf) stream_last();
+    } else {
+      if (ktail && j == cur.ns - 1 && cur.ns > cur.nf) stream_ragged();
+    }
     static_for<NL>([&](auto Q) { copy_one(Q, (uint32_t)(j * kStageBytes)); });
   }
   asm volatile("s_waitcnt vmcnt(%0)" : : "n"((NSTAGE - 1) * NL) : "memory");      // slab 0 landed
@@ -687,8 +692,13 @@ void wide_tile_kernel(const Plan) {
       if (kt == k_switch) {
         more = piece_of(it + 1, nxt);
         p = words.now();
-        if (more) stream_piece(nxt);
-        else stream_end();
+        if constexpr (kOneSlab) {
+          if (more) stream_piece(nxt);
+          else stream_end();
+        } else {
+          if (more) stream_to(nxt);
+          else stream_end();
+        }
         if (tracked && has_in) {
           p = words.now();
           in_here(place());
@@ -700,8 +710,13 @@ void wide_tile_kernel(const Plan) {
         }
       }
       // the slab copied next is the last one of the stream's piece, and ragged
-      if ((ktail || (kOneSlab && one_slab)) && (kt == k_switch - 1 || (kt == last && more && nxt.ns == NSTAGE)) && (kt < k_switch ? cur.ns > cur.nf : nxt.ns > nxt.nf))
-        stream_last();
+      if constexpr (kOneSlab) {
+        if ((ktail || one_slab) && (kt == k_switch - 1 || (kt == last && more && nxt.ns == NSTAGE)) && (kt < k_switch ? cur.ns > cur.nf : nxt.ns > nxt.nf))
+          stream_last();
+      } else {
+        if (ktail && (kt == k_switch - 1 || (kt == last && more && nxt.ns == NSTAGE)) && (kt < k_switch ? cur.ns > cur.nf : nxt.ns > nxt.nf))
+          stream_ragged();
+      }
       // the next barrier something is to be done behind, or whose wait is another one
       int stop = kt < k_switch ? (ktail && kt < k_switch - 1 ? k_switch - 1 : k_switch) : (NSTAGE > 2 && kt < last - 1 ? kt + 1 : last);
       if (kt < NSTAGE && (counting || (NSTAGE > 2 && it > 0))) stop = min(stop, kt + 1);
