@@ -485,6 +485,8 @@ t3_status launch_gemm(int mode, const t3k::Plan &q, int32_t tm, int32_t tn, bool
 
 // ---- products in 8 bits
 constexpr int32_t kMaxK8 = 131056;     // (K of 131072 times -128 -128 is 2^31)
+constexpr int64_t kFarLd = 1ll << 32;  // leading dimensions from which products with a number of rows might not be 64-bit numbers
+constexpr int64_t kFarStride = 1ll << 48;
 inline bool aligned4(const void *q) { return (reinterpret_cast<uintptr_t>(q) & 3u) == 0; }
 
 // What a call in 8 bits has to check beside make_plan, and the problem as make_plan takes it: A and B in pairs of int8, which are where
@@ -501,7 +503,7 @@ t3_status pairs_of(const t3_problem *p, bool fused, const float *scale_a, const 
   if (fused && ((p->flags & T3_FLAG_TWO_WRITERS) || p->split_k > 1)) return T3_ERR_UNSUPPORTED;
   if (p->lda < p->K || p->ldb < p->K) return T3_ERR_BAD_SHAPE;
   if (p->K % 16 || p->lda % 16 || p->ldb % 16 || !aligned4(scale_a) || !aligned4(scale_b)) return T3_ERR_ALIGN;
-  if (p->K > kMaxK8) return T3_ERR_UNSUPPORTED;
+  if (p->K > kMaxK8 || p->lda >= kFarLd || p->ldb >= kFarLd) return T3_ERR_UNSUPPORTED;
   // ranges of whole ring steps (a range that cuts one is in tracked tiles, which the kernels here do not work in)
   const int64_t tpc = ceil_div(p->M, tm) * ceil_div(p->N / p->tp, tn), T = tpc * p->tp;
   const int64_t limit = p->tile_limit < 0 || p->tile_limit > T ? T : p->tile_limit, begin = p->tile_begin < 0 ? 0 : p->tile_begin;
@@ -523,9 +525,10 @@ t3_status check_grouped(const t3_grouped *g, bool wgrad, int size) {
   const bool kn = g->b_layout == T3_B_KN;
   const int64_t b_rows = kn ? g->K : g->N, b_cols = kn ? g->N : g->K;
   if (g->lda < g->K || g->ldb < b_cols || g->ldc < g->N || g->stride_b < 0) return T3_ERR_BAD_SHAPE;
-  if (wgrad && g->groups > 1 && b_rows && g->stride_b < (b_rows - 1) * g->ldb + b_cols) return T3_ERR_BAD_SHAPE;
+  if (wgrad && g->groups > 1 && b_rows && g->ldb < kFarLd && g->stride_b < (b_rows - 1) * g->ldb + b_cols) return T3_ERR_BAD_SHAPE;
   if (g->flags & ~(wgrad ? T3_GROUPED_ACCUMULATE : 0u)) return T3_ERR_UNSUPPORTED;
   if (g->groups > T3_MAX_GROUPS || (size == 1 && (kn || g->K > kMaxK8))) return T3_ERR_UNSUPPORTED;
+  if (g->lda >= kFarLd || g->ldb >= kFarLd || g->ldc >= kFarLd || g->stride_b >= kFarStride) return T3_ERR_UNSUPPORTED;
   const int per = 16 / size;                     // elements of 16 bytes
   if (g->K % per || g->lda % per) return T3_ERR_ALIGN;
   if (wgrad) {
@@ -755,6 +758,7 @@ t3_status t3_quant_rows(int32_t rows, int32_t cols, int32_t x_type, const void *
   if (!x || !q || !scale) return T3_ERR_NULL;
   const bool f32 = x_type == T3_TYPE_F32;
   if (cols % 8 || ldx % (f32 ? 4 : 8) || ldq % 8 || !aligned16(x) || (reinterpret_cast<uintptr_t>(q) & 7u) || !aligned4(scale)) return T3_ERR_ALIGN;
+  if (ldx >= kFarLd || ldq >= kFarLd) return T3_ERR_UNSUPPORTED;
   if (!rows) return T3_OK;
   // a wavefront per row of up to four pieces a lane, else a workgroup; as many pieces as the row has
   const bool wave = cols <= 8 * 64 * 4;

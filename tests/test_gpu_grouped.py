@@ -159,6 +159,34 @@ def test_no_contraction_and_no_rows():
     assert bool((C[:5] == 0.0).all()) and bool((C[5] == OUTSIDE).all())
 
 
+def test_groups_further_apart_than_32_bits_count():
+    """The second group's operand (and gradient) starts past 2^31 elements and 2^32 bytes."""
+    N, K, rows, counts, stride = 64, 128, 40, [25, 15], (1 << 32) + 4096
+    g, o = gen(6), offsets_of([25, 15])
+    raw = torch.empty(2 * (stride + N * K), dtype=torch.int8, device=DEV)
+    A, d = bf16(g, rows, K), bf16(g, rows, N)
+    w = [bf16(g, N, K) for _ in counts]
+    B = raw.view(torch.bfloat16)
+    for e in range(2):
+        B[e * stride:e * stride + N * K] = w[e].view(-1)
+    C = torch.zeros((rows, N), device=DEV)
+    t3.t3_gemm_grouped(t3.grouped(rows, 2, N, K, stride_b=stride), device(o), A, B, C)
+    for e, (a, b) in enumerate(spans(o, rows)):
+        close(C[a:b], A[a:b].double() @ w[e].double().t(), sum_bound(A[a:b], w[e].t()))
+    q = [torch.randint(-128, 128, (N, K), generator=g, device=DEV, dtype=torch.int8) for _ in counts]
+    x = torch.randint(-128, 128, (rows, K), generator=g, device=DEV, dtype=torch.int8)
+    sa, sb = torch.ones(rows, device=DEV), torch.ones((2, N), device=DEV)
+    for e in range(2):
+        raw[e * stride:e * stride + N * K] = q[e].view(-1)
+    t3.t3_gemm_grouped_i8(t3.grouped(rows, 2, N, K, stride_b=stride), device(o), x, sa, raw, sb, C)
+    for e, (a, b) in enumerate(spans(o, rows)):
+        close(C[a:b], *product8(x[a:b], sa[a:b], q[e], sb[e]))
+    dB, apart = raw.view(torch.float32), (1 << 30) + 1024
+    t3.t3_gemm_grouped_wgrad(t3.grouped(rows, 2, N, K, stride_b=apart), device(o), A, d, dB)
+    for e, (a, b) in enumerate(spans(o, rows)):
+        close(dB[e * apart:e * apart + N * K].view(N, K), d[a:b].double().t() @ A[a:b].double(), sum_bound(d[a:b].t(), A[a:b]))
+
+
 BAD = [[5, 2, 30, 30], [-4, 10, 10, 25], [0, 10, 2000000000, 3], [-2147483648, 2147483647, 0, 40], [40, 30, 20, 10], [3, 0, 0, 0]]
 
 

@@ -28,6 +28,7 @@ def test_rows_refused():
     assert quant(rows=-1) == quant(cols=-8) == quant(ldx=56) == quant(ldq=56) == quant(x_type=2) == t3.T3_ERR_BAD_SHAPE
     assert quant(cols=60, ldx=64, ldq=64) == quant(ldx=68) == quant(ldq=68) == quant(x=FAKE + 2) == quant(q=FAKE + 4) == quant(s=FAKE + 2) == t3.T3_ERR_ALIGN
     assert quant(ldx=66, x_type=t3.T3_TYPE_F32) == t3.T3_ERR_ALIGN
+    assert quant(rows=1 << 30, ldx=1 << 61) == quant(rows=1 << 30, ldq=1 << 61) == t3.T3_ERR_UNSUPPORTED
 
 
 GEMM = dict(M=256, N=1024, K=256, tp=4, rank=0, tile_m=128, tile_n=128)
@@ -51,6 +52,7 @@ def test_products_in_8_bits_refused(call):
     assert call(b_layout=t3.T3_B_KN, ldb=1024) == call(a_layout=t3.T3_A_KM, lda=256) == call(K=131072) == t3.T3_ERR_UNSUPPORTED
     assert call(tile_begin=1) == call(tile_limit=5) == t3.T3_ERR_UNSUPPORTED      # (16 tiles a ring step)
     assert call(M=1 << 20, K=4096) == t3.T3_ERR_UNSUPPORTED                        # A of 2^32 bytes
+    assert call(lda=1 << 60) == call(ldb=1 << 60) == t3.T3_ERR_UNSUPPORTED         # (times M no 64-bit number)
     lib = t3.lib()
     assert lib.t3_gemm_i8(None, FAKE, FAKE, FAKE, FAKE, FAKE, 0) == t3.T3_ERR_NULL
     assert lib.t3_gemm_rs_fused_i8(None, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 0) == t3.T3_ERR_NULL
@@ -86,6 +88,7 @@ def test_groups_refused(call):
     assert call(groups=257) == call(flags=2) == t3.T3_ERR_UNSUPPORTED
     assert call(K=124) == call(N=62) == call(lda=130) == call(ldc=66) == call(ldb=130) == call(stride_b=64 * 128 + 2) == t3.T3_ERR_ALIGN
     assert call(o=FAKE + 2) == call(A=FAKE + 8) == call(B=FAKE + 8) == call(C=FAKE + 8) == t3.T3_ERR_ALIGN
+    assert call(lda=1 << 60) == call(ldb=1 << 60) == call(ldc=1 << 60) == call(stride_b=1 << 60) == t3.T3_ERR_UNSUPPORTED
     assert call(rows=1 << 25, K=256) == call(rows=1 << 25, N=64, ldc=128) == t3.T3_ERR_UNSUPPORTED or call is grouped8
     assert call(N=0) == t3.T3_OK
 
