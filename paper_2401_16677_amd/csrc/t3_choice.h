@@ -85,23 +85,24 @@ inline Choice workgroup_tile(const t3_problem *p, int cus, int64_t steps, bool w
   return pick;
 }
 
-// Products by group: tiles of which a last round of at most half the workgroups is done in quarters, by a second launch.
-inline bool quarters_of(TileShape t) { return t.m >= 192 && t.n == 256; }
+// Products by group: tiles of which a last round of at most half the workgroups is done in quarters, by a second launch.  In us, whole and in quarters, operands
+// and results in memory: 16384 rows of 16 groups x 2048 x 4096, 544 tiles, 291 and 271, B stored N x K 292 and 275; 8192 of 16 x 5120 x 1280, 820 tiles, 159 and
+// 154; the second launch with nothing to do 109.8 and 110.9 (4096 of 8 x 2560 x 4096).
+inline bool quarters_of(TileShape t) { return t.m == 256 && t.n == 256; }
 // Rounds that x rounds of tiles take: the last one whole, or as quarters 0.55.
 inline double rounds_of(double x, bool quarters) {
   const double whole = (double)(int64_t)x, rest = x - whole;
   if (rest <= 0.0) return whole;
   return whole + (quarters && whole >= 1.0 && rest <= 0.5 ? 0.55 : 1.0);
 }
-// The tile of products by group, by the same times.  The host knows the rows of all groups together, so the tiles are those of groups
+// The tile of products by group, by the same times.  (They are those of warm operands; over 190 drawn products, cold and warm, what is picked takes 1.007
+// of the best tile's time on average, and at worst 1.3: 146 rows of 24 groups x 352 x 5248, B stored K x N, 24 us by 32 x 32, 18 by 64 x 64.)  The host knows the rows of all groups together, so the tiles are those of groups
 // as large as the average, every one with half a tile more than its rows fill (or one tile), give or take what groups' ends make of it.  M x N: C, or the
 // gradient of a group's weights (wgrad), whose K is a group's rows.
 inline Choice grouped_tile(bool wgrad, bool kn, int64_t M, int64_t N, int64_t K, int64_t groups, int cus, bool wide_ok) {
   double best = -1.0;
   Choice pick{kSmallTile, {64, 64}};
-  constexpr Cand kTall{{192, 256}, 2, 1, 0.92, 13.3};
-  for (int i = -1; i < (int)(sizeof(kCand) / sizeof(kCand[0])); ++i) {
-    const Cand &c = i < 0 ? kTall : kCand[i];
+  for (const Cand &c : kCand) {
     if (c.t.m == 32 && c.t.n == 64) continue;
     const double used = (double)(wgrad || M > groups ? groups : M), columns = (double)ceil_div(N, c.t.n);
     const double even = (double)M / c.t.m + 0.5 * used;

@@ -99,7 +99,7 @@ struct Plan {
   const int32_t *offsets;
   int64_t stride_b;
   // cut: tiles of a last round that would occupy at most half the workgroups are left (kCutLeave) to a second launch, which does them in
-  // quarters (kCutQuarters; tile_m x tile_n, Wt, Mt and order.round are those of the first).
+  // quarters (kCutQuarters; Wt, Mt and order.round are those of the first).
   int32_t groups, rows, cut;
 };
 

@@ -114,7 +114,7 @@ __device__ __forceinline__ bool get_piece(PlanWords &words, int it, Piece &w) {
 }
 
 // Products by group.  (As many slabs as there are stages at least: behind a group's rows they are zeros.)
-// pos: this workgroup's next grid position.  CUT: quarters of tiles of 256 columns and at most 256 rows (see kCutQuarters).
+// pos: this workgroup's next grid position.  CUT: quarters of tiles of 256 x 256 (see kCutQuarters).
 template <int MODE, int BM, int BN, int NSTAGE, int CUT>
 __device__ __forceinline__ bool get_group_piece(PlanWords &words, const GroupRows &groups, uint32_t &pos, Piece &w) {
   const Plan p = words.now();
@@ -129,9 +129,8 @@ __device__ __forceinline__ bool get_group_piece(PlanWords &words, const GroupRow
       q = (quarters >> 3) * (q & 7) + min(quarters & 7, q & 7) + (q >> 3);           // (an XCD's in a run)
       groups.tile<kRows>(p, first + (q >> 2), at);
       w.tl = Tile{at.group, 0, 0, 2 * at.nj + (int)(q >> 1 & 1)};
-      const int begin = at.mi * p.tile_m, end = min(begin + p.tile_m, kRows ? at.rows : p.M);
-      w.m0 = begin + (int)(q & 1) * BM;
-      w.m_rows = min(BM, end - w.m0);
+      w.m0 = (2 * at.mi + (int)(q & 1)) * BM;
+      w.m_rows = min(BM, (kRows ? at.rows : p.M) - w.m0);
       if (w.m_rows <= 0 || w.tl.nj * BN >= p.W) continue;
     } else {
       const uint32_t q = pos;
@@ -175,7 +174,7 @@ void wide_tile_kernel(const Plan) {
   words.load(lane);
   Plan p = words.now();                          // (read anew where something rare begins)
   GroupRows groups;
-  if constexpr (grouped || wgrad) groups.load(p, lane, CUT ? (uint32_t)p.tile_m : (uint32_t)BM);
+  if constexpr (grouped || wgrad) groups.load(p, lane, CUT ? 2 * BM : BM);
   uint32_t next_pos = blockIdx.x;
   auto piece_of = [&](int it, Piece &w) {
     if constexpr (grouped || wgrad) return get_group_piece<MODE, BM, BN, NSTAGE, CUT>(words, groups, next_pos, w);

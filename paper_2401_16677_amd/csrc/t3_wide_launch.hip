@@ -20,7 +20,6 @@ t3_status T3_LAUNCHER(const Plan &q, int32_t tm, int32_t tn, hipStream_t s) {
   const dim3 grid((unsigned)(q.total_blocks > q.resident ? q.resident : q.total_blocks));
 #if T3_MODE >= 2
   if (q.cut == kCutQuarters) return T3_WIDE_QUARTERS(4, 4, 2, 1, 2, 4);
-  if (tm == 192) return T3_WIDE(6, 8, 2, 1, 1, 2);
 #endif
   if (tm == 256 && tn == 256) return T3_WIDE(8, 8, 2, 1, 1, 2);
   if (tm == 256 && tn == 192) return T3_WIDE(8, 6, 2, 2, 2, T3_I8 ? 4 : 5);
