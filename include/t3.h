@@ -337,7 +337,7 @@ t3_status t3_ag_step(const t3_problem *p, int32_t step, const float *upstream_R,
 /*
  * Where a launch's time goes (a measuring aid for Sec. 4.1's overlap: how much of a tile's time
  * is reduction traffic and how much is matrix work).  While `stamps` is set, every launch of
- * the tile kernels (t3_gemm_rs_fused, t3_gemm_rs_fused_static, t3_gemm), from any thread,
+ * the tile kernels (t3_gemm_rs_fused, t3_gemm_rs_fused_static, t3_gemm, their 8-bit forms and the products by group), from any thread,
  * records for workgroup w and its i-th piece of work (a tile, or half of one in a balanced
  * tail), i < T3_TIMELINE_ITEMS, four readings of the device's 100 MHz wall clock at
  * stamps[(w * T3_TIMELINE_ITEMS + i) * 4 + 0 .. 3]:
@@ -425,6 +425,8 @@ typedef struct {
  *   offsets  int32 [groups + 1], device
  *   A        bf16 [rows][lda], B bf16 at B + e stride_b, by b_layout; lda, ldb, stride_b and K multiples of 8
  *   C        fp32 [rows][ldc], N and ldc multiples of 4; out: the groups' rows
+ * The same problem and offsets give the same bits, under graph capture as well.  A call is one launch, or two (a last round of tiles that
+ * would leave most of the device idle is done in smaller ones); `offsets` may change between calls and replays, not during one.
  * T3_B_KN is the gradient to the rows of a layer whose weights are stored N x K (K and N trade places): N a multiple of 8.  A and a group's B below 2^31 elements each, C below 2^32 bytes.
  */
 t3_status t3_gemm_grouped(const t3_grouped *g, const int32_t *offsets, const void *A, const void *B, float *C,
