@@ -141,9 +141,10 @@ def grouped(rows, groups, N, K, b_layout=T3_B_NK, lda=None, ldb=None, ldc=None, 
 
 def _dptr(t):
     """Device (or NULL) address of a torch tensor / raw int / None, as the foreign call takes it."""
-    if t is None or isinstance(t, int):
+    try:                                           # (a tensor, nearly always)
+        return t.data_ptr()
+    except AttributeError:
         return t
-    return t.data_ptr()
 
 
 # torch.cuda.current_stream() builds a Stream object through several layers of Python (4 of the

@@ -95,7 +95,7 @@ inline double rounds_of(double x, bool quarters) {
   if (rest <= 0.0) return whole;
   return whole + (quarters && whole >= 1.0 && rest <= 0.5 ? 0.55 : 1.0);
 }
-// The tile of products by group, by the same times.  (They are those of warm operands; over 190 drawn products, cold and warm, what is picked takes 1.007
+// The tile of products by group, by the same times.  (They are those of warm operands; over 190 drawn products, cold and warm, what is picked takes 1.02
 // of the best tile's time on average, and at worst 1.3: 146 rows of 24 groups x 352 x 5248, B stored K x N, 24 us by 32 x 32, 18 by 64 x 64.)  The host knows the rows of all groups together, so the tiles are those of groups
 // as large as the average, every one with half a tile more than its rows fill (or one tile), give or take what groups' ends make of it.  M x N: C, or the
 // gradient of a group's weights (wgrad), whose K is a group's rows.

@@ -5,11 +5,17 @@
 namespace t3k {
 namespace {
 
+template <int BM, int MODE, int BKN, int AKM, int I8>
+t3_status launch_tiles(const Plan &q, hipStream_t s) {
+  const dim3 grid((unsigned)q.total_blocks), block(256);
+  // (the plan by one vector request while all workgroups are on the chip at once: see small_tile_kernel)
+  if (q.total_blocks <= q.resident * (BM == 32 ? 2 : 1)) return launch(small_tile_kernel<BM, BM, 4, 2, MODE, BKN, AKM, true, I8>, grid, block, s, q);
+  return launch(small_tile_kernel<BM, BM, 4, 2, MODE, BKN, AKM, false, I8>, grid, block, s, q);
+}
 template <int MODE, int BKN, int AKM, int I8>
 t3_status launch_small(const Plan &q, int32_t tm, int32_t tn, hipStream_t s) {
-  const dim3 grid((unsigned)q.total_blocks), block(256);
-  if (tm == 64 && tn == 64) return launch(small_tile_kernel<64, 64, 4, 2, MODE, BKN, AKM, false, I8>, grid, block, s, q);
-  return tm == 32 && tn == 32 ? launch(small_tile_kernel<32, 32, 4, 2, MODE, BKN, AKM, false, I8>, grid, block, s, q) : T3_ERR_UNSUPPORTED;
+  if (tm == 64 && tn == 64) return launch_tiles<64, MODE, BKN, AKM, I8>(q, s);
+  return tm == 32 && tn == 32 ? launch_tiles<32, MODE, BKN, AKM, I8>(q, s) : T3_ERR_UNSUPPORTED;
 }
 
 }  // namespace
