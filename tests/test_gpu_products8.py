@@ -108,6 +108,26 @@ def test_product_strides_chunks_and_columns_beside(M, N, K, tp):
     assert bool((c[:, N:] == 5.0).all())
 
 
+# a last round of at most half the workgroups of 256 x 192 and 256 x 256: its tiles in halves of K
+@pytest.mark.parametrize("M,N,K", [(1000, 16640, 1040), (2040, 10240, 2064), (1000, 20484, 1040)])
+def test_product_of_a_split_last_round(M, N, K):
+    g = gen(K)
+    a, b, sa, sb = int8(g, M, K), int8(g, N, K), scales(g, M), scales(g, N)
+    c, p = torch.full((M, N), 5.0, device=DEV), t3.problem(M, N, K, 1, 0)
+    want, bound = product8(a, sa, b, sb)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        t3.t3_gemm_i8(p, a, sa, b, sb, c)
+    for i in range(4):                              # eager and replayed calls in turn, with the same flags between the halves
+        c.fill_(5.0)
+        if i % 2:
+            graph.replay()
+        else:
+            t3.t3_gemm_i8(p, a, sa, b, sb, c)
+        torch.cuda.synchronize()
+        close(c, want, bound)
+
+
 def test_product_at_its_limits():
     """The largest sum of the longest K, no K, no rows, scales of zero and of no number."""
     K = 131056
@@ -132,6 +152,7 @@ FUSED = [(24, 1152, 1152, 16, 9, 0, (0, 0)), (100, 320, 400, 4, 3, t3.T3_FLAG_FW
          (257, 1040, 640, 2, 0, t3.T3_FLAG_FWD_BF16 | t3.T3_FLAG_FWD_DIRECT, (0, 0)), (520, 2144, 336, 4, 1, t3.T3_FLAG_FWD_BF16, (256, 128)),
          (1000, 2128, 1072, 4, 2, t3.T3_FLAG_STEP0_STORE_ONLY, (128, 256)), (2040, 5120, 1040, 5, 2, t3.T3_FLAG_FWD_DIRECT, (256, 256)),
          (1100, 3200, 576, 8, 7, t3.T3_FLAG_FWD_DIRECT | t3.T3_FLAG_STEP0_STORE_ONLY, (0, 0)), (700, 1504, 2000, 2, 1, 0, (0, 0)), (64, 64, 32, 1, 0, 0, (0, 0)),
+         (1000, 16640, 1040, 5, 3, t3.T3_FLAG_FWD_DIRECT, (0, 0)), (2040, 10240, 2064, 8, 0, 0, (256, 256)),
          (2000, 4096, 112, 4, 1, t3.T3_FLAG_FWD_DIRECT, (256, 256)), (2300, 4256, 128, 8, 5, 0, (0, 0))]
 
 
