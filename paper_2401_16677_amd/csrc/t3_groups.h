@@ -39,6 +39,8 @@ struct GroupRows {
   static constexpr int kSets = kMaxGroups / 64;
   uint32_t end[kSets], tiles[kSets];   // lane l of set r, group 64 r + l: behind its last row; rows of tiles up to and with it
   uint32_t first, all_tiles;           // first row of the first group; rows of tiles of all groups
+  bool sorted = false;                 // contractions over rows: the groups are taken in the order of by_length
+  uint32_t by_length = 0;
 
   // bm: rows of a tile
   __device__ __forceinline__ void load(const Plan &p, int lane, uint32_t bm) {
@@ -67,6 +69,22 @@ struct GroupRows {
       }
     }
     all_tiles = count;
+  }
+  // Contractions over a group's rows: the groups by length, the longest first, where there is more than a round of tiles, so that those of a round take about as
+  // long as one another and the last ones are short.  Lane r then has the r-th group: it is behind as many as have a larger key.  (In us, in the order
+  // that the groups are in, shortest first and longest first: 8190 rows of 16 groups x 5120 x 1280 177, 190 and 165; 16384 of 32 x 2048 x 1024 132, 120 and 122; 16000 of
+  // 8 x 2560 x 2560 226, 245 and 212.  More than 64 groups are left as they are: their tiles are short ones.)
+  __device__ __forceinline__ void longest_first(const Plan &p, int lane) {
+    sorted = p.groups <= 64 && (uint32_t)p.tpc * (uint32_t)p.groups > p.order.round;
+    if (!sorted) return;
+    const uint32_t rows = end[0] - dpp<0x138, 0xf>(first, end[0]);
+    const uint32_t key = min(rows, (1u << 26) - 1) << 6 | (uint32_t)(63 - lane);       // (no two alike; behind the last group no rows)
+    uint32_t before = 0u;
+    for (int g = 0; g < p.groups; g += 8) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) before += __builtin_amdgcn_readlane(key, g + i) > key ? 1u : 0u;
+    }
+    by_length = (uint32_t)__builtin_amdgcn_ds_permute((int)(lane < p.groups ? before : (uint32_t)lane) * 4, lane);
   }
   __device__ __forceinline__ static uint32_t of(const uint32_t (&a)[kSets], int g) {
     uint32_t v = __builtin_amdgcn_readlane(a[0], g & 63);
@@ -127,7 +145,7 @@ struct GroupRows {
   }
   __device__ __forceinline__ void tile_of_all(const Plan &p, uint32_t at, GroupTile &t) const {
     const uint32_t g = div_by(at, p.by_tpc);
-    rows_of((int)g, t);
+    rows_of((int)(sorted ? __builtin_amdgcn_readlane(by_length, g & 63) : g), t);
     in_group(at - g * (uint32_t)p.tpc, (uint32_t)p.Mt, (uint32_t)p.Wt, t);
   }
 };

@@ -175,6 +175,7 @@ void wide_tile_kernel(const Plan) {
   Plan p = words.now();                          // (read anew where something rare begins)
   GroupRows groups;
   if constexpr (grouped || wgrad) groups.load(p, lane, CUT ? 2 * BM : BM);
+  if constexpr (wgrad) groups.longest_first(p, lane);
   uint32_t next_pos = blockIdx.x;
   auto piece_of = [&](int it, Piece &w) {
     if constexpr (grouped || wgrad) return get_group_piece<MODE, BM, BN, NSTAGE, CUT>(words, groups, next_pos, w);

@@ -306,6 +306,21 @@ def test_wgrad_large(N, K, counts):
     check_wgrad(counts, 0, 3, N, K, True, True, False)
 
 
+# several rounds of tiles, whose groups the launch takes by their lengths: like ones, empty ones, one that has nearly all rows, and more than it sorts
+BY_LENGTH = [([125] * 64, 1024, 1024), ([0] * 20 + [1, 5000, 2] + [64] * 10, 2048, 1024), ([7 * i % 190 for i in range(17)], 1288, 1032),
+             (list(range(65)), 2048, 2048), ([90 - i for i in range(64)], 1024, 768), ([0] * 17, 1288, 1032)]
+
+
+@pytest.mark.parametrize("layout", ["nk", "kn"])
+@pytest.mark.parametrize("case", range(len(BY_LENGTH)))
+def test_wgrad_of_several_rounds(case, layout):
+    counts, N, K = BY_LENGTH[case]
+    M, n = (K, N) if layout == "kn" else (N, K)
+    wide, tm, tn, _ = grouped_tile(True, True, M, n, sum(counts) + 6, len(counts))
+    assert wide and len(counts) * -(-M // tm) * -(-n // tn) > 256
+    check_wgrad(counts, 4, 2, N, K, layout == "kn", bool(case % 2), case % 3 == 0)
+
+
 # ------------------------------------------------------------------ together
 
 def test_layer_of_experts_and_its_gradients():
