@@ -769,8 +769,15 @@ t3_status t3_quant_rows(int32_t rows, int32_t cols, int32_t x_type, const void *
     return held <= 2 ? t3k::quant_rows_kernel<256, 2, kF32> : (held <= 4 ? t3k::quant_rows_kernel<256, 4, kF32> : t3k::quant_rows_kernel<256, t3k::kQuantPieces, kF32>);
   };
   auto kernel = f32 ? pick(std::true_type{}) : pick(std::false_type{});
-  return launch(kernel, dim3((unsigned)(wave ? ceil_div(rows, 4) : rows)), dim3(256), static_cast<hipStream_t>(stream), x, ldx, q, ldq, scale,
-                rows, cols);
+  // (a launch has less than 2^32 lanes: 2^23 workgroups at a time)
+  const int64_t part = (wave ? 4ll : 1ll) << 23;
+  for (int64_t at = 0; at < rows; at += part) {
+    const int32_t here = (int32_t)(rows - at < part ? rows - at : part);
+    const t3_status st = launch(kernel, dim3((unsigned)(wave ? ceil_div(here, 4) : here)), dim3(256), static_cast<hipStream_t>(stream),
+                                static_cast<const void *>(static_cast<const char *>(x) + at * ldx * (f32 ? 4 : 2)), ldx, q + at * ldq, ldq, scale + at, here, cols);
+    if (st != T3_OK) return st;
+  }
+  return T3_OK;
 }
 
 t3_status t3_gemm_i8(const t3_problem *p, const int8_t *A, const float *scale_a, const int8_t *B, const float *scale_b, float *C,

@@ -7,6 +7,7 @@ namespace {
 
 template <int BM, int MODE, int BKN, int AKM, int I8>
 t3_status launch_tiles(const Plan &q, hipStream_t s) {
+  if (q.total_blocks >= 1 << 24) return T3_ERR_UNSUPPORTED;      // (a launch has less than 2^32 lanes)
   const dim3 grid((unsigned)q.total_blocks), block(256);
   // (the plan by one vector request while all workgroups are on the chip at once: see small_tile_kernel)
   if (q.total_blocks <= q.resident * (BM == 32 ? 2 : 1)) return launch(small_tile_kernel<BM, BM, 4, 2, MODE, BKN, AKM, true, I8>, grid, block, s, q);

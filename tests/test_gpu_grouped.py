@@ -306,6 +306,16 @@ def test_wgrad_large(N, K, counts):
     check_wgrad(counts, 0, 3, N, K, True, True, False)
 
 
+def test_wgrad_of_more_tiles_than_a_launch_has_is_refused():
+    N, K, E = 1 << 24, 8, 64
+    assert grouped_tile(True, True, N, K, 4, E, wide_ok=False)[0] is False     # (rows of 32 MB)
+    dB = torch.empty((E, N, K), device=DEV)
+    with pytest.raises(t3.T3Error) as e:
+        t3.t3_gemm_grouped_wgrad(t3.grouped(4, E, N, K), device([0] * E + [4]), torch.zeros((4, K), dtype=torch.bfloat16, device=DEV),
+                                 torch.zeros((4, N), dtype=torch.bfloat16, device=DEV), dB)
+    assert e.value.status == t3.T3_ERR_UNSUPPORTED
+
+
 # several rounds of tiles, whose groups the launch takes by their lengths: like ones, empty ones, one that has nearly all rows, and more than it sorts
 BY_LENGTH = [([125] * 64, 1024, 1024), ([0] * 20 + [1, 5000, 2] + [64] * 10, 2048, 1024), ([7 * i % 190 for i in range(17)], 1288, 1032),
              (list(range(65)), 2048, 2048), ([90 - i for i in range(64)], 1024, 768), ([0] * 17, 1288, 1032)]

@@ -65,6 +65,20 @@ def test_rows_borders(dtype, top):
     assert np.array_equal(q, want_q) and np.array_equal(s, want_s)
 
 
+def test_rows_of_several_launches():
+    """More rows than a launch has wavefronts for, and rows without columns."""
+    rows, g = (1 << 25) + 5, gen(2)
+    x = torch.randn((rows, 8), generator=g, device=DEV).to(torch.bfloat16)
+    q, s = torch.full((rows + 1, 8), 99, dtype=torch.int8, device=DEV), torch.full((rows + 1,), 7.0, device=DEV)
+    t3.t3_quant_rows(rows, 8, x, q, s)
+    for at in (slice(0, 9), slice((1 << 25) - 9, rows)):
+        want_q, want_s = rows8(x[at].double().cpu().numpy())
+        assert np.array_equal(q[at].cpu().numpy(), want_q) and np.array_equal(s[at].cpu().numpy(), want_s)
+    assert bool((q[:rows].abs().amax(1) == 127).all()) and bool((q[rows] == 99).all()) and float(s[rows]) == 7.0
+    t3.t3_quant_rows(3, 0, x, q, s, ldx=8, ldq=8)
+    assert s[:4].tolist() == [0.0, 0.0, 0.0, float(rows8(x[3:4].double().cpu().numpy())[1][0])]
+
+
 def test_rows_that_are_no_numbers():
     x = torch.ones((5, 72), device=DEV)
     x[1, 3], x[2, 70], x[3, 0], x[4] = float("nan"), float("inf"), float("-inf"), 0.0
