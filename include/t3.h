@@ -374,7 +374,10 @@ t3_status t3_timeline(uint64_t *stamps, int64_t words);
  *   x      [rows][ldx], t3_type: bf16 (ldx a multiple of 8) or fp32 (of 4), read
  *   q      [rows][ldq], ldq a multiple of 8, out: columns [0, cols); 8-byte aligned
  *   scale  [rows], out
- * cols a multiple of 8 (T3_ERR_ALIGN); x 16-byte, scale 4-byte aligned.
+ * cols a multiple of 8 (T3_ERR_ALIGN); x 16-byte, scale 4-byte aligned.  No rows: T3_OK, nothing is launched.
+ *
+ * In this call, the products in 8 bits and those by group an array without elements may be NULL (no rows: A, C and what else has
+ * as many; no columns; K of 0), as may one that then nothing is read of.
  */
 typedef enum { T3_TYPE_BF16 = 0, T3_TYPE_F32 = 1 } t3_type;
 t3_status t3_quant_rows(int32_t rows, int32_t cols, int32_t x_type, const void *x, int64_t ldx, int8_t *q, int64_t ldq,
@@ -439,7 +442,7 @@ t3_status t3_gemm_grouped_i8(const t3_grouped *g, const int32_t *offsets, const 
 
 /*
  * The gradient of the groups' weights: dB_e = the sum over group e's rows r of dC[r] (x) A[r], in the layout of B (NK:
- * dB_e[n][k] = sum dC[r][n] A[r][k]).  A group without rows has a gradient of zeros.
+ * dB_e[n][k] = sum dC[r][n] A[r][k]).  A group without rows has a gradient of zeros, and so have all groups if `rows` is 0.
  *
  *   A   bf16 [rows][lda], dC bf16 [rows][ldc]; lda, ldc, N and K multiples of 8
  *   dB  fp32 at dB + e stride_b, leading dimension ldb, both multiples of 4, groups not overlapping; out, or with

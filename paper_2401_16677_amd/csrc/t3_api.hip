@@ -280,11 +280,13 @@ t3_status make_plan(const t3_problem *p, t3k::Call call, int need, const void *A
   const bool fused_like = (need & kNeedTrack) != 0;
   const bool direct = fused_like && (p->flags & T3_FLAG_FWD_DIRECT);
   const bool two_writers = fused_like && (p->flags & T3_FLAG_TWO_WRITERS);
-  if ((need & kNeedAB) && (!A || !B)) return T3_ERR_NULL;
-  if ((need & kNeedR) && !R) return T3_ERR_NULL;
-  if ((need & kNeedC) && !C) return T3_ERR_NULL;
+  // (in 8 bits an array without elements needs no address)
+  const bool some = !i8 || (p->M && p->N);
+  if ((need & kNeedAB) && some && (!i8 || p->K) && (!A || !B)) return T3_ERR_NULL;
+  if ((need & kNeedR) && some && !R) return T3_ERR_NULL;
+  if ((need & kNeedC) && some && !C) return T3_ERR_NULL;
   if ((need & kNeedTrack) && !track) return T3_ERR_NULL;
-  if ((need & kNeedFwd) && p->tp > 1 && !fwd && !(two_writers && (need & kNeedAB)))
+  if ((need & kNeedFwd) && some && p->tp > 1 && !fwd && !(two_writers && (need & kNeedAB)))
     return T3_ERR_NULL;                         // (the fused call releases nothing with two writers)
   if (p->flags & ~(T3_FLAG_STEP0_STORE_ONLY | T3_FLAG_FWD_DIRECT | T3_FLAG_TWO_WRITERS |
                    T3_FLAG_FWD_BF16))
@@ -494,7 +496,7 @@ inline bool aligned4(const void *q) { return (reinterpret_cast<uintptr_t>(q) & 3
 t3_status pairs_of(const t3_problem *p, bool fused, const float *scale_a, const float *scale_b, t3_problem *pairs) {
   t3_status st = check_shape(p);
   if (st != T3_OK) return st;
-  if (!scale_a || !scale_b) return T3_ERR_NULL;
+  if (p->M && p->N && (!scale_a || !scale_b)) return T3_ERR_NULL;
   int32_t tm, tn;
   st = resolve_tile(p, &tm, &tn);
   if (st != T3_OK) return st;
@@ -581,9 +583,11 @@ t3_status grouped_product(const t3_grouped *g, bool i8, const int32_t *offsets, 
                           const float *scale_b, float *C, void *stream) {
   t3_status st = check_grouped(g, false, i8 ? 1 : 2);
   if (st != T3_OK) return st;
-  if (!offsets || !A || !B || !C || (i8 && (!scale_a || !scale_b))) return T3_ERR_NULL;
+  // (arrays without elements need no address, nor do those that nothing is read of: a rank that got no rows has none)
+  const bool some = g->rows && g->N;
+  if (!offsets || (some && (!C || (i8 && (!scale_a || !scale_b)))) || (some && g->K && (!A || !B))) return T3_ERR_NULL;
   if (!aligned4(offsets) || !aligned16(A) || !aligned16(B) || !aligned16(C) || (i8 && (!aligned4(scale_a) || !aligned4(scale_b)))) return T3_ERR_ALIGN;
-  if (!g->rows || !g->N) return T3_OK;
+  if (!some) return T3_OK;
   const int per = i8 ? 2 : 1;
   t3k::Plan q{};
   q.A = static_cast<const uint16_t *>(A);
@@ -755,7 +759,7 @@ t3_status t3_gemm(const t3_problem *p, const void *A, const void *B, float *C, v
 t3_status t3_quant_rows(int32_t rows, int32_t cols, int32_t x_type, const void *x, int64_t ldx, int8_t *q, int64_t ldq, float *scale,
                         void *stream) {
   if (rows < 0 || cols < 0 || (x_type != T3_TYPE_BF16 && x_type != T3_TYPE_F32) || ldx < cols || ldq < cols) return T3_ERR_BAD_SHAPE;
-  if (!x || !q || !scale) return T3_ERR_NULL;
+  if (rows && (!scale || (cols && (!x || !q)))) return T3_ERR_NULL;
   const bool f32 = x_type == T3_TYPE_F32;
   if (cols % 8 || ldx % (f32 ? 4 : 8) || ldq % 8 || !aligned16(x) || (reinterpret_cast<uintptr_t>(q) & 7u) || !aligned4(scale)) return T3_ERR_ALIGN;
   if (ldx >= kFarLd || ldq >= kFarLd) return T3_ERR_UNSUPPORTED;
@@ -828,9 +832,10 @@ t3_status t3_gemm_grouped_i8(const t3_grouped *g, const int32_t *offsets, const 
 t3_status t3_gemm_grouped_wgrad(const t3_grouped *g, const int32_t *offsets, const void *A, const void *dC, float *dB, void *stream) {
   t3_status st = check_grouped(g, true, 2);
   if (st != T3_OK) return st;
-  if (!offsets || !A || !dC || !dB) return T3_ERR_NULL;
+  const bool some = g->N && g->K;                // (no rows: gradients of zeros, made of no A and no dC)
+  if (!offsets || (some && !dB) || (some && g->rows && (!A || !dC))) return T3_ERR_NULL;
   if (!aligned4(offsets) || !aligned16(A) || !aligned16(dC) || !aligned16(dB)) return T3_ERR_ALIGN;
-  if (!g->N || !g->K) return T3_OK;
+  if (!some) return T3_OK;
   const bool kn = g->b_layout == T3_B_KN;        // the result's rows are the columns of: A (else dC)
   t3k::Plan q{};
   q.A = static_cast<const uint16_t *>(kn ? A : dC);

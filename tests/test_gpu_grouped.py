@@ -420,3 +420,52 @@ def test_same_inputs_same_bits_on_other_streams_and_in_a_graph_with_new_offsets(
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(t, r) for t, r in zip(b, want[i]))
+
+
+# ------------------------------------------------------------------ a rank that got no rows
+
+@pytest.mark.parametrize("layout", ["nk", "kn"])
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("N,K,E,wide", [(24, 40, 3, False), (1032, 520, 9, True)])
+def test_wgrad_of_no_rows(N, K, E, wide, add, layout):
+    """Tensors of no rows have no address; all gradients are zeros, or unchanged where they are added to."""
+    kn = layout == "kn"
+    M, n = (K, N) if kn else (N, K)
+    assert grouped_tile(True, True, M, n, 0, E)[0] == wide
+    A, dC = (torch.empty((0, c), dtype=torch.bfloat16, device=DEV) for c in (K, N))
+    assert A.data_ptr() == 0 and dC.data_ptr() == 0
+    dB = torch.randn((E + 1, M, n), generator=gen(N), device=DEV)
+    old = dB.clone()
+    p = t3.grouped(0, E, N, K, b_layout=t3.T3_B_KN if kn else t3.T3_B_NK, flags=t3.T3_GROUPED_ACCUMULATE if add else 0)
+    t3.t3_gemm_grouped_wgrad(p, device([0] * (E + 1)), A, dC, dB)
+    torch.cuda.synchronize()
+    assert torch.equal(dB[:E], old[:E] if add else torch.zeros_like(old[:E])) and torch.equal(dB[E], old[E])
+
+
+def test_layer_of_no_rows_and_products_of_no_contraction():
+    E, N, K, off = 3, 64, 128, device([0] * 4)
+    x, y, c = (torch.empty((0, w), dtype=d, device=DEV) for w, d in ((K, torch.bfloat16), (N, torch.bfloat16), (N, torch.float32)))
+    q, s = torch.empty((0, K), dtype=torch.int8, device=DEV), torch.empty(0, device=DEV)
+    w, w8, sw = bf16(gen(0), E, N, K), torch.ones((E, N, K), dtype=torch.int8, device=DEV), torch.ones((E, N), device=DEV)
+    t3.t3_quant_rows(0, K, x, q, s)
+    t3.t3_gemm_grouped(t3.grouped(0, E, N, K), off, x, w, c)
+    t3.t3_gemm_grouped(t3.grouped(0, E, K, N, b_layout=t3.T3_B_KN), off, y, w, torch.empty((0, K), device=DEV))
+    t3.t3_gemm_grouped_i8(t3.grouped(0, E, N, K), off, q, s, w8, sw, c)
+    t3.t3_gemm_i8(t3.problem(0, N, K, 1, 0), q, s, w8, sw, c)
+    # no contraction: products of zeros, of operands that have no address
+    C = torch.full((6, N), OUTSIDE, device=DEV)
+    for i8 in (False, True):
+        C.fill_(OUTSIDE)
+        none, one = torch.empty((6, 0), dtype=torch.int8 if i8 else torch.bfloat16, device=DEV), torch.ones(max(6, E * N), device=DEV)
+        if i8:
+            t3.t3_gemm_grouped_i8(t3.grouped(6, E, N, 0), device([1, 2, 2, 5]), none, one, none, one, C)
+        else:
+            t3.t3_gemm_grouped(t3.grouped(6, E, N, 0), device([1, 2, 2, 5]), none, none, C)
+        torch.cuda.synchronize()
+        assert bool((C[1:5] == 0.0).all()) and bool((C[:1] == OUTSIDE).all()) and bool((C[5:] == OUTSIDE).all())
+    C.fill_(OUTSIDE)
+    t3.t3_gemm_i8(t3.problem(6, N, 0, 1, 0), none, one, none, one, C)
+    s0 = torch.full((3,), OUTSIDE, device=DEV)
+    t3.t3_quant_rows(2, 0, torch.empty((2, 0), dtype=torch.bfloat16, device=DEV), torch.empty((2, 0), dtype=torch.int8, device=DEV), s0)
+    torch.cuda.synchronize()
+    assert bool((C == 0.0).all()) and s0.tolist() == [0.0, 0.0, OUTSIDE]

@@ -3,6 +3,7 @@ import ctypes
 
 import numpy as np
 import pytest
+import torch
 
 from paper_2401_16677_amd import binding as t3
 from products import rows8, spans
@@ -117,3 +118,21 @@ def test_the_tests_own_reading_of_rows_and_offsets():
     assert q.tolist() == [[127, 0, 2, -2], [0] * 4, [0] * 4] and s[0] == 1.0 and s[1] == 0.0 and np.isnan(s[2])
     assert spans([5, 2, 30, 30], 40) == [(5, 5), (5, 30), (30, 30)]
     assert spans([-4, 10, 2000000000, 3], 25) == [(0, 10), (10, 25), (25, 25)]
+
+
+def test_arrays_without_elements_need_no_address():
+    """A rank that got no rows has tensors without elements, whose address is 0."""
+    none = [torch.empty(s, dtype=d) for s, d in [((0, 64), torch.bfloat16), ((0, 64), torch.int8), ((0,), torch.float32), ((0, 64), torch.float32)]]
+    x, q, s, c = none
+    assert all(t.data_ptr() == 0 for t in none)
+    for y, t in ((x, t3.T3_TYPE_BF16), (c, t3.T3_TYPE_F32)):
+        assert quant(rows=0, x=y, q=q, s=s, x_type=t) == t3.T3_OK
+    assert plain(M=0, A=q, sa=s, C=c) == fused(M=0, A=q, sa=s, R=c, fwd=c) == t3.T3_OK
+    assert plain(N=0, B=q, sb=s, C=c) == fused(N=0, B=q, sb=s, R=c, fwd=c) == t3.T3_OK
+    assert grouped(rows=0, A=x, C=c) == grouped8(rows=0, A=q, sa=s, C=c) == t3.T3_OK
+    assert grouped(N=0, B=x, C=c) == grouped8(N=0, B=q, sb=s, C=c) == t3.T3_OK
+    assert wgrad(N=0, B=c, C=x) == wgrad(K=0, A=x, B=c) == t3.T3_OK
+    # what has elements, or is written without any rows, is asked for still
+    assert quant(cols=0, x=None, q=None, s=None) == plain(K=0, A=None, B=None, C=None) == plain(K=0, A=None, B=None, sa=None) == t3.T3_ERR_NULL
+    assert fused(M=0, track=None) == grouped(rows=0, o=None) == wgrad(N=0, o=None) == t3.T3_ERR_NULL
+    assert grouped(K=0, A=None, B=None, C=None) == grouped8(K=0, A=None, B=None, sa=None) == wgrad(rows=0, A=None, C=None, B=None) == t3.T3_ERR_NULL
