@@ -59,12 +59,12 @@ class T3Error(RuntimeError):
 
 
 _lib = None
-_float32 = None                                    # torch.float32, once torch is loaded
+_bfloat16 = _float32 = None                        # torch's, once it is loaded
 
 
 def lib():
     """Load libt3.so (built in-tree by paper_2401_16677_amd.build).  Raises if it is missing."""
-    global _lib, _float32
+    global _lib, _bfloat16, _float32
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise FileNotFoundError(
@@ -73,7 +73,7 @@ def lib():
         # streams.  PyTorch ships its own copy, so it is loaded first and libt3.so's
         # dependency on libamdhip64 resolves to that one.
         import torch
-        _float32 = torch.float32
+        _bfloat16, _float32 = torch.bfloat16, torch.float32
         L = ctypes.CDLL(LIB_PATH)
         vp, i32, i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
         pp = ctypes.POINTER(T3Problem)
@@ -251,8 +251,11 @@ def t3_gemm(p, A, B, C, stream=None):
 
 def t3_quant_rows(rows, cols, x, q, scale, ldx=None, ldq=None, x_type=None, stream=None):
     L = lib()
-    if x_type is None:                             # a tensor's own type
-        x_type = T3_TYPE_F32 if getattr(x, "dtype", None) is _float32 else T3_TYPE_BF16
+    if x_type is None:                             # a tensor's own type; an address alone: bf16
+        dtype = getattr(x, "dtype", _bfloat16)
+        if dtype is not _bfloat16 and dtype is not _float32:
+            raise TypeError(f"t3_quant_rows takes rows of bfloat16 or float32, not {dtype}")
+        x_type = T3_TYPE_BF16 if dtype is _bfloat16 else T3_TYPE_F32
     _check(L.t3_quant_rows(rows, cols, x_type, _dptr(x), cols if ldx is None else ldx, _dptr(q),
                                cols if ldq is None else ldq, _dptr(scale), _stream(stream)),
            "t3_quant_rows")

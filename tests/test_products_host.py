@@ -136,3 +136,14 @@ def test_arrays_without_elements_need_no_address():
     assert quant(cols=0, x=None, q=None, s=None) == plain(K=0, A=None, B=None, C=None) == plain(K=0, A=None, B=None, sa=None) == t3.T3_ERR_NULL
     assert fused(M=0, track=None) == grouped(rows=0, o=None) == wgrad(N=0, o=None) == t3.T3_ERR_NULL
     assert grouped(K=0, A=None, B=None, C=None) == grouped8(K=0, A=None, B=None, sa=None) == wgrad(rows=0, A=None, C=None, B=None) == t3.T3_ERR_NULL
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float64, torch.int8, torch.int16, torch.int32])
+def test_rows_of_other_types_are_refused(dtype):
+    """(Read as bfloat16 they would give integers and scales of other numbers.)"""
+    x = torch.zeros((4, 64), dtype=dtype)
+    with pytest.raises(TypeError, match=str(dtype)):
+        t3.t3_quant_rows(0, 64, x, FAKE, FAKE, stream=0)
+    for ok in (torch.bfloat16, torch.float32):
+        t3.t3_quant_rows(0, 64, x.to(ok), FAKE, FAKE, stream=0)
+    t3.t3_quant_rows(0, 64, FAKE, FAKE, FAKE, stream=0)
