@@ -610,8 +610,7 @@ t3_status grouped_product(const t3_grouped *g, bool i8, const int32_t *offsets, 
   DeviceFacts dev;
   st = device_facts(&dev);
   if (st != T3_OK) return st;
-  // (the wide-tile kernel's limits, see wide_fits)
-  const bool wide_ok = 256 * q.lda * 2 <= 1ll << 31 && (kn ? q.K : 256) * q.ldb * 2 <= 1ll << 31 && 256 * q.ldc * 4 <= 1ll << 31;
+  const bool wide_ok = t3k::grouped_wide_fits(kn, q.K, q.lda, q.ldb, q.ldc);
   const t3k::Choice c = t3k::grouped_tile(false, kn, g->rows, g->N, q.K, g->groups, dev.cus, wide_ok);
   const int32_t tm = c.tile.m, tn = c.tile.n;
   // rows of tiles: every group may end with a tile of its own that is not full, and has no more tiles than rows
@@ -855,9 +854,7 @@ t3_status t3_gemm_grouped_wgrad(const t3_grouped *g, const int32_t *offsets, con
   DeviceFacts dev;
   st = device_facts(&dev);
   if (st != T3_OK) return st;
-  // (the wide-tile kernel's limits, see wide_fits: a group's rows, and the slabs of zeros behind them)
-  const int64_t k_rows = (int64_t)g->rows + 4 * 64;
-  const bool wide_ok = k_rows * q.lda * 2 <= 1ll << 31 && k_rows * q.ldb * 2 <= 1ll << 31 && 256 * q.ldc * 4 <= 1ll << 31;
+  const bool wide_ok = t3k::wgrad_wide_fits(g->rows, q.lda, q.ldb, q.ldc);
   const t3k::Choice c = t3k::grouped_tile(true, true, q.M, q.N, g->rows, g->groups, dev.cus, wide_ok);
   const int32_t tm = c.tile.m, tn = c.tile.n;
   q.Mt = (int32_t)ceil_div(q.M, tm);

@@ -186,6 +186,18 @@ inline bool wide_fits(const t3_problem *p, int64_t ld_out) {
          (p->b_layout == T3_B_KN ? p->K : rows) * p->ldb * 2 <= kMost && rows * ld_out * 4 <= kMost;
 }
 
+// The same for products by group.  A slab's lanes address 64 k-rows of an operand stored K x ..., the last slab's too, of which those past K have to
+// come out past the buffer: all of them, not K alone, stay below 2^31 bytes, or they would lie among the marked offsets, or be inside the buffer again
+// (8 rows of 2^26 elements: k-row 32 starts at byte 2^32).  wgrad: K is a group's rows, and slabs of zeros are behind them.
+inline bool grouped_wide_fits(bool kn, int64_t K, int64_t lda, int64_t ldb, int64_t ldc) {
+  const int64_t kMost = 1ll << 31, rows = 256, k_rows = K > 64 ? ceil_div(K, 64) * 64 : 64;
+  return rows * lda * 2 <= kMost && (kn ? k_rows : rows) * ldb * 2 <= kMost && rows * ldc * 4 <= kMost;
+}
+inline bool wgrad_wide_fits(int64_t group_rows, int64_t lda, int64_t ldb, int64_t ldc) {
+  const int64_t kMost = 1ll << 31, rows = 256, k_rows = group_rows + 4 * 64;
+  return k_rows * lda * 2 <= kMost && k_rows * ldb * 2 <= kMost && rows * ldc * 4 <= kMost;
+}
+
 // Where a launch of the wide-tile kernel lets a chunk's tile columns start so that R's (the plain GEMM's C's) rows are cut at
 // 64-byte granules: chunk c starts (c W) mod 16 columns into a granule, and its tiles but the first start as many columns
 // early.  15, or 0: they start at multiples of the tile.  Only where that costs no further tile (the last tile has the columns

@@ -8,3 +8,5 @@ extern "C" void grouped_tile(int wgrad, int kn, int64_t M, int64_t N, int64_t K,
   out[2] = c.tile.n;
   out[3] = t3k::quarters_of(c.tile);
 }
+
+extern "C" int grouped_wide_fits(int kn, int64_t K, int64_t lda, int64_t ldb, int64_t ldc) { return t3k::grouped_wide_fits(kn, K, lda, ldb, ldc); }

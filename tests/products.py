@@ -76,3 +76,11 @@ def quarters(counts, N, tile, places=256):
     """(tiles of the groups, those of the last round that are done in quarters)"""
     T = sum(-(-n // tile[0]) for n in counts) * -(-N // tile[1])
     return T, T % places if T > places and 2 * (T % places) <= places else 0
+
+
+def grouped_wide_fits(kn, K, lda, ldb, ldc):
+    """Whether the wide-tile kernel's offsets reach all of a forward product by group."""
+    import ctypes
+    grouped_tile(False, kn, 1, 8, 8, 1)               # (built)
+    _choice.grouped_wide_fits.argtypes = [ctypes.c_int] + [ctypes.c_int64] * 4
+    return bool(_choice.grouped_wide_fits(int(kn), K, lda, ldb, ldc))

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2401_16677_amd import binding as t3
-from products import HALF, MORE, close, grouped_tile, product8, quarters, rows8, spans
+from products import HALF, MORE, close, grouped_tile, grouped_wide_fits, product8, quarters, rows8, spans
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -469,3 +469,18 @@ def test_layer_of_no_rows_and_products_of_no_contraction():
     t3.t3_quant_rows(2, 0, torch.empty((2, 0), dtype=torch.bfloat16, device=DEV), torch.empty((2, 0), dtype=torch.int8, device=DEV), s0)
     torch.cuda.synchronize()
     assert bool((C == 0.0).all()) and s0.tolist() == [0.0, 0.0, OUTSIDE]
+
+
+@pytest.mark.parametrize("ldb,wide", [(1 << 24, True), (1 << 25, False), (1 << 26, False)])
+def test_short_contraction_of_far_rows(ldb, wide):
+    """Eight k-rows of B far from one another: the others of a slab are zeros, not rows that are there (an infinity times A's zeros would be NaN)."""
+    K, counts = 8, [700, 900, 1, 450, 0, 1300]
+    N, rows, g, o = 2600, sum(counts), gen(1), offsets_of(counts)
+    assert grouped_wide_fits(True, K, K, ldb, N) == wide and grouped_tile(False, True, rows, N, K, len(counts))[0]
+    A = torch.randint(1, 9, (rows, K), generator=g, device=DEV).to(torch.bfloat16)
+    B = torch.zeros((K, ldb), dtype=torch.bfloat16, device=DEV)
+    B[:, :N] = torch.randint(-8, 9, (K, N), generator=g, device=DEV).to(torch.bfloat16)
+    B[0, 5::64], B[7, 9::64] = float("inf"), -float("inf")
+    C = torch.full((rows, N), OUTSIDE, device=DEV)
+    t3.t3_gemm_grouped(t3.grouped(rows, len(counts), N, K, b_layout=t3.T3_B_KN, ldb=ldb, stride_b=0), device(o), A, B, C)
+    assert torch.equal(C.double(), A.double() @ B[:, :N].double())

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2401_16677_amd import binding as t3
-from products import rows8, spans
+from products import grouped_wide_fits, rows8, spans
 
 FAKE = 0x10000
 
@@ -147,3 +147,22 @@ def test_rows_of_other_types_are_refused(dtype):
     for ok in (torch.bfloat16, torch.float32):
         t3.t3_quant_rows(0, 64, x.to(ok), FAKE, FAKE, stream=0)
     t3.t3_quant_rows(0, 64, FAKE, FAKE, FAKE, stream=0)
+
+
+@pytest.mark.parametrize("cols", [256, 128])
+def test_lanes_behind_a_short_contraction_stay_past_the_buffer(cols):
+    """B stored K x N: the byte offsets of a slab's 64 k-rows, as the wide-tile kernel's 32-bit numbers, where it may be used: k-rows from K on, and
+    columns from the tile's last on, are past the buffer (an infinity there times A's zeros would be NaN)."""
+    fits = 0
+    for K in (8, 16, 24, 56, 64):
+        for ldb in [1 << e for e in range(12, 29)] + [(1 << 24) + 8, (1 << 25) - 8, 3 << 23, 5 << 24]:
+            if K * ldb >= 1 << 31 or not grouped_wide_fits(True, K, K, ldb, 512):
+                continue
+            fits += 1
+            k, col = np.arange(64, dtype=np.uint64)[:, None], np.arange(0, 256, 8, dtype=np.uint64)[None, :]
+            off = (k * np.uint64(ldb) + col) * np.uint64(2) & np.uint64(0xFFFFFFFF)
+            if cols < 256:                         # (lanes outside get the top bit, the others lose it)
+                off = np.where(col >= cols, off | np.uint64(1 << 31), off & np.uint64((1 << 31) - 1))
+            inside = off < K * ldb * 2
+            assert np.array_equal(inside, np.broadcast_to((k < K) & (col < cols), inside.shape)), (K, ldb)
+    assert fits > 50 and grouped_wide_fits(True, 64, 64, 1 << 24, 512) and not grouped_wide_fits(True, 65, 72, 1 << 24, 512)
