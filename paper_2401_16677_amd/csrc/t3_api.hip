@@ -542,9 +542,7 @@ t3_status check_grouped(const t3_grouped *g, bool wgrad, int size) {
   // (B's in the gradient of a group)
   if (g->rows * g->lda >= (1ll << 32) / size || g->rows * g->ldc >= (wgrad ? 1ll << 31 : 1ll << 30) || b_rows * g->ldb >= (wgrad ? 1ll << 30 : (1ll << 32) / size))
     return T3_ERR_UNSUPPORTED;
-  // tiles, 32 x 32 the smallest, fit 31 bits
-  const int64_t most = wgrad ? ceil_div(b_rows, 32) * ceil_div(b_cols, 32) * g->groups : (ceil_div(g->rows, 32) + g->groups) * ceil_div(g->N, 32);
-  if (most >= (1ll << 31) - 8) return T3_ERR_UNSUPPORTED;
+  // (so tiles, 32 x 32 the smallest, are less than 2^31: at most 256 gradients of 2^22, or 2^27 of a result's)
   return T3_OK;
 }
 
@@ -851,10 +849,11 @@ t3_status t3_gemm_grouped_wgrad(const t3_grouped *g, const int32_t *offsets, con
   q.offsets = offsets;
   q.stride_b = g->stride_b;
   q.groups = g->groups;
+  const bool wide_ok = t3k::wgrad_wide_fits(g->rows, q.lda, q.ldb, q.ldc);
+  if (!wide_ok && ceil_div(q.M, 64) * ceil_div(q.N, 64) * g->groups >= 1 << 24) return T3_ERR_UNSUPPORTED;
   DeviceFacts dev;
   st = device_facts(&dev);
   if (st != T3_OK) return st;
-  const bool wide_ok = t3k::wgrad_wide_fits(g->rows, q.lda, q.ldb, q.ldc);
   const t3k::Choice c = t3k::grouped_tile(true, true, q.M, q.N, g->rows, g->groups, dev.cus, wide_ok);
   const int32_t tm = c.tile.m, tn = c.tile.n;
   q.Mt = (int32_t)ceil_div(q.M, tm);

@@ -50,7 +50,7 @@ struct Plan {
   uint32_t *track;
   int64_t lda, ldb, ldr, ldc;
   int64_t limit;     // tiles with issue index >= limit do nothing
-  int64_t begin;     // nor do tiles with issue index < begin
+  int64_t begin;     // nor do tiles with issue index < begin.  By group, small-tile kernel: the launch's first grid position
   int32_t M, N, K, P, rank, W, own;
   // The grid of WORKGROUP tiles: rows, columns, tiles per chunk.  `begin` and `limit` are counted
   // in these.  Where the launch covers whole ring steps they are cut as suits the chip, whatever

@@ -7,7 +7,18 @@ namespace {
 
 template <int BM, int MODE, int BKN, int AKM, int I8>
 t3_status launch_tiles(const Plan &q, hipStream_t s) {
-  if (q.total_blocks >= 1 << 24) return T3_ERR_UNSUPPORTED;      // (a launch has less than 2^32 lanes)
+  // (a launch has less than 2^32 lanes: 2^23 workgroups at a time, `begin` the first one's grid position)
+  constexpr int32_t kPart = 1 << 23;
+  if (q.total_blocks > kPart) {
+    Plan part = q;
+    for (int32_t at = 0; at < q.total_blocks; at += kPart) {
+      part.begin = at;
+      part.total_blocks = q.total_blocks - at < kPart ? q.total_blocks - at : kPart;
+      const t3_status st = launch(small_tile_kernel<BM, BM, 4, 2, MODE, BKN, AKM, false, I8>, dim3((unsigned)part.total_blocks), dim3(256), s, part);
+      if (st != T3_OK) return st;
+    }
+    return T3_OK;
+  }
   const dim3 grid((unsigned)q.total_blocks), block(256);
   // (the plan by one vector request while all workgroups are on the chip at once: see small_tile_kernel)
   if (q.total_blocks <= q.resident * (BM == 32 ? 2 : 1)) return launch(small_tile_kernel<BM, BM, 4, 2, MODE, BKN, AKM, true, I8>, grid, block, s, q);

@@ -57,7 +57,7 @@ __global__ __launch_bounds__(64 * WK) void small_tile_kernel(const Plan arg) {
     GroupRows g;
     g.load(p, lane, BM);
     GroupTile at;
-    if (!g.tile_of_position<grouped>(p, blockIdx.x, at)) return;
+    if (!g.tile_of_position<grouped>(p, (uint32_t)p.begin + blockIdx.x, at)) return;
     tl = Tile{0, 0, at.mi, at.nj};
     if (grouped) {
       row_lo = at.row0;

@@ -484,3 +484,32 @@ def test_short_contraction_of_far_rows(ldb, wide):
     C = torch.full((rows, N), OUTSIDE, device=DEV)
     t3.t3_gemm_grouped(t3.grouped(rows, len(counts), N, K, b_layout=t3.T3_B_KN, ldb=ldb, stride_b=0), device(o), A, B, C)
     assert torch.equal(C.double(), A.double() @ B[:, :N].double())
+
+
+# ------------------------------------------------------------------ more workgroups than one launch has lanes for
+
+def test_forward_of_several_launches():
+    counts = [1, 0, 2] * 60 + [1] * 75
+    N, K, E, rows = 4194300, 8, len(counts), sum(counts)
+    wide, tm, tn, _ = grouped_tile(False, False, rows, N, K, E, wide_ok=grouped_wide_fits(False, K, K, K, N))
+    assert not wide and sum(-(-n // tm) for n in counts) * -(-N // tn) > 1 << 24
+    g, o = gen(4), offsets_of(counts)
+    A, B = (torch.randint(-8, 9, (n, K), generator=g, device=DEV).to(torch.bfloat16) for n in (rows, N))
+    C = torch.full((rows, N), OUTSIDE, device=DEV)
+    t3.t3_gemm_grouped(t3.grouped(rows, E, N, K, stride_b=0), device(o), A, B, C)
+    for c in range(0, N, 1 << 18):                    # (whole numbers: exact)
+        assert torch.equal(C[:, c:c + (1 << 18)], A.float() @ B[c:c + (1 << 18)].float().t()), c
+
+
+@pytest.mark.parametrize("add", [False, True])
+def test_wgrad_of_several_launches(add):
+    N, K, E = 1 << 23, 8, 64
+    M, n, counts = N, K, [0] * 30 + [3] + [0] * 32 + [1]
+    wide, tm, tn, _ = grouped_tile(True, True, M, n, 4, E, wide_ok=False)
+    assert not wide and E * (M // tm) >= 1 << 24 > E * (M // 64)
+    g, o = gen(5), offsets_of(counts)
+    A, dC = (torch.randint(-8, 9, (4, w), generator=g, device=DEV).to(torch.bfloat16) for w in (K, N))
+    dB = torch.full((E, N, K), 3.0, device=DEV)
+    t3.t3_gemm_grouped_wgrad(t3.grouped(4, E, N, K, flags=t3.T3_GROUPED_ACCUMULATE if add else 0), device(o), A, dC, dB)
+    for e, (a, b) in enumerate(spans(o, 4)):
+        assert torch.equal(dB[e], dC[a:b].float().t() @ A[a:b].float() + (3.0 if add else 0.0)), e

@@ -166,3 +166,18 @@ def test_lanes_behind_a_short_contraction_stay_past_the_buffer(cols):
             inside = off < K * ldb * 2
             assert np.array_equal(inside, np.broadcast_to((k < K) & (col < cols), inside.shape)), (K, ldb)
     assert fits > 50 and grouped_wide_fits(True, 64, 64, 1 << 24, 512) and not grouped_wide_fits(True, 65, 72, 1 << 24, 512)
+
+
+def test_limits_of_groups_are_ones_of_sizes():
+    """What the header says of sizes, whatever tiles are picked; no further limit (without a GPU a launch that is not refused ends in T3_ERR_HIP)."""
+    launched = (t3.T3_OK, t3.T3_ERR_HIP)
+    far = dict(N=1 << 24, K=8, ldc=1 << 24)           # rows of dC of 2^25 bytes
+    assert wgrad(rows=300, groups=64, **far) == t3.T3_ERR_UNSUPPORTED          # dC of 2^31 elements and more
+    assert wgrad(rows=0, groups=64, N=8, K=1 << 24, lda=1 << 24) == t3.T3_ERR_UNSUPPORTED     # 2^24 tiles of 64 x 64, (rows + 256) lda 2^32
+    if torch.cuda.is_available():
+        return
+    assert wgrad(rows=4, groups=63, **far) in launched                         # (2^24 less 2^18 of them)
+    assert wgrad(rows=4, groups=64, **{**far, "N": (1 << 24) - 64}) in launched
+    assert grouped(rows=255, groups=256, N=4194300, K=8, stride_b=0) in launched
+    assert grouped(rows=1, groups=256, N=(1 << 28) - 8, K=8, ldb=8, stride_b=0) in launched
+    assert grouped(rows=(1 << 28) - 8, groups=256, N=4, K=8) in launched
