@@ -350,6 +350,8 @@ t3_status t3_ag_step(const t3_problem *p, int32_t step, const float *upstream_R,
  *   3  the results have been handed to the memory system (they are acknowledged later, while
  *      the next piece starts); the hand-ordered kernel has added the incoming partial on the
  *      way, and has the next piece's first slabs in LDS
+ * A product by group whose last round of tiles is done in smaller ones records these behind the full rounds: w is then a workgroup of the second launch, which has up to
+ * twice as many of them, and i counts the first launch's rounds.
  * Workgroups w >= words / (4 * T3_TIMELINE_ITEMS) record nothing, nor do launches on workgroup
  * tiles of less than 128 rows, nor launches on 256 x 256 tiles that the hand-ordered kernel does
  * not serve.  Entries a launch does not

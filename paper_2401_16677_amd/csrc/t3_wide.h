@@ -234,6 +234,7 @@ void wide_tile_kernel(const Plan) {
   auto stamp = [&](int it, int k) {
     if (!timeline) return;
     p = words.now();
+    if constexpr (CUT) it += (int)div_by(groups.uncut(p, groups.count<grouped>(p)), p.order.by_round);   // (behind the full rounds of the first launch)
     if (wave == 0 && (int)blockIdx.x < p.timeline_wgs && it < kTimelineItems) {
       const uint64_t now = wall_clock64();
       __builtin_amdgcn_raw_buffer_store_b64(u32x2{(uint32_t)now, (uint32_t)(now >> 32)},

@@ -513,3 +513,52 @@ def test_wgrad_of_several_launches(add):
     t3.t3_gemm_grouped_wgrad(t3.grouped(4, E, N, K, flags=t3.T3_GROUPED_ACCUMULATE if add else 0), device(o), A, dC, dB)
     for e, (a, b) in enumerate(spans(o, 4)):
         assert torch.equal(dB[e], dC[a:b].float().t() @ A[a:b].float() + (3.0 if add else 0.0)), e
+
+
+# ------------------------------------------------------------------ timeline
+
+@pytest.mark.parametrize("counts,cut", ROUNDS)
+@pytest.mark.parametrize("call", ["nk", "kn", "8 bits"])
+def test_timeline_of_two_launches(call, counts, cut):
+    """Every tile leaves four readings, those of the last round that are done in quarters behind the full rounds; results are the same."""
+    N, K, rows, E, kn = 6144, 1024, sum(counts), len(counts), call == "kn"
+    T, left = quarters(counts, N, (256, 256))
+    assert left == cut and grouped_tile(False, kn, rows, N, K, E)[1:] == (256, 256, True)
+    g, off = gen(11), device(offsets_of(counts))
+    p = t3.grouped(rows, E, N, 2 * K if call == "8 bits" else K, b_layout=t3.T3_B_KN if kn else t3.T3_B_NK)
+    if call == "8 bits":
+        A, B = (torch.randint(-128, 128, (n, 2 * K), generator=g, device=DEV, dtype=torch.int8) for n in (rows, E * N))
+        sa, sb = torch.ones(rows, device=DEV), torch.ones(E * N, device=DEV)
+    else:
+        A, B = bf16(g, rows, K), bf16(g, E, *((K, N) if kn else (N, K)))
+
+    def run(C):
+        if call == "8 bits":
+            t3.t3_gemm_grouped_i8(p, off, A, sa, B, sb, C)
+        else:
+            t3.t3_gemm_grouped(p, off, A, B, C)
+        torch.cuda.synchronize()
+        return C
+
+    want = run(torch.zeros((rows, N), device=DEV))
+    items = t3.T3_TIMELINE_ITEMS
+    st = torch.full((520, items, 4), -1, dtype=torch.int64, device=DEV)
+    t3.t3_timeline(st)
+    try:
+        got = run(torch.zeros((rows, N), device=DEV))
+    finally:
+        t3.t3_timeline(None)
+    assert torch.equal(got, want)
+    st = st.cpu()
+    taken = (st != -1).all(dim=2)
+    assert torch.equal(taken, (st != -1).any(dim=2))
+    rounds, last = (T - left) // 256, (T - left) % 256
+    assert bool(taken[:256, :rounds].all()) and int(taken[256:, :rounds].sum()) == 0
+    if left:
+        # quarters of the last tiles that hold rows (N is whole tiles): half of a group's last tile may be none
+        assert last == 0 and 2 * left <= int(taken[:, rounds].sum()) <= 4 * left and int(taken[:, rounds + 1:].sum()) == 0
+    else:
+        assert int(taken[:, rounds].sum()) == last and int(taken[:, rounds + 1:].sum()) == 0
+    for w in range(520):
+        readings = st[w][taken[w]].flatten().tolist()
+        assert readings == sorted(readings), w
