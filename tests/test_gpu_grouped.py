@@ -562,3 +562,30 @@ def test_timeline_of_two_launches(call, counts, cut):
     for w in range(520):
         readings = st[w][taken[w]].flatten().tolist()
         assert readings == sorted(readings), w
+
+
+# ------------------------------------------------------------------ more groups than a wavefront has lanes, on the largest tiles
+
+# groups, the lengths' modulus, tiles of the last round that are done in quarters (of the last groups)
+MANY = [(65, 487, 124), (100, 521, 96), (128, 509, 40), (129, 509, 48), (193, 401, 28), (256, 509, 12)]
+
+
+@pytest.mark.parametrize("layout", ["nk", "kn", "8 bits"])
+@pytest.mark.parametrize("E,mod,cut", MANY)
+def test_more_than_64_groups_on_the_largest_tiles(E, mod, cut, layout):
+    counts = [(37 * i * i + 11 * i) % mod for i in range(E)]
+    N, K, rows, kn = 1024, 1024, sum(counts) + 3, layout == "kn"
+    assert counts[0] == 0 and grouped_tile(False, kn, rows, N, K, E) == (True, 256, 256, True)
+    assert quarters(counts, N, (256, 256))[1] == cut
+    if layout != "8 bits":
+        check_forward(counts, 1, 2, N, K, kn, integers=E % 2 == 0)
+        return
+    g, o = gen(E), offsets_of(counts, 1)
+    A = torch.randint(-128, 128, (rows, 2 * K), generator=g, device=DEV, dtype=torch.int8)
+    B = torch.randint(-128, 128, (E, N, 2 * K), generator=g, device=DEV, dtype=torch.int8)
+    sa, sb = torch.exp(torch.randn(rows, generator=g, device=DEV)), torch.exp(torch.randn((E, N), generator=g, device=DEV))
+    C = torch.full((rows, N), OUTSIDE, device=DEV)
+    t3.t3_gemm_grouped_i8(t3.grouped(rows, E, N, 2 * K), device(o), A, sa, B, sb, C)
+    for e, (a, b) in enumerate(spans(o, rows)):
+        close(C[a:b], *product8(A[a:b], sa[a:b], B[e], sb[e]))
+    assert bool((C[:1] == OUTSIDE).all()) and bool((C[o[-1]:] == OUTSIDE).all())
