@@ -25,8 +25,10 @@
  *    set of flags, created at first use); and the pointer given to t3_timeline.
  *  - `stream` is a hipStream_t passed as void* (NULL = the default stream).  Calls are
  *    asynchronous on that stream and never synchronise it.
- *  - Arguments are validated on the host before anything is enqueued; on any status
- *    other than T3_OK nothing was launched and no buffer was touched.
+ *  - Arguments are validated on the host before anything is enqueued: a call that returns another status
+ *    than T3_OK and T3_ERR_HIP has launched nothing and touched no buffer.  After T3_ERR_HIP (the runtime refused a
+ *    launch) that holds for calls of one launch; one of several (t3_gemm_rs_fused_static; t3_quant_rows and the products by group
+ *    where they say so) may have made the first of them, and what it writes is undefined.
  *  - A and B are read only.  Buffers must not overlap each other.
  */
 #ifndef T3_H
@@ -376,7 +378,8 @@ t3_status t3_timeline(uint64_t *stamps, int64_t words);
  *   x      [rows][ldx], t3_type: bf16 (ldx a multiple of 8) or fp32 (of 4), read
  *   q      [rows][ldq], ldq a multiple of 8, out: columns [0, cols); 8-byte aligned
  *   scale  [rows], out
- * cols a multiple of 8 (T3_ERR_ALIGN); x 16-byte, scale 4-byte aligned.  No rows: T3_OK, nothing is launched.
+ * cols a multiple of 8 (T3_ERR_ALIGN); x 16-byte, scale 4-byte aligned.  No rows: T3_OK, nothing is launched.  More than 2^23 rows (2^25 of at
+ * most 2048 columns): several launches.
  *
  * In this call, the products in 8 bits and those by group an array without elements may be NULL (no rows: A, C and what else has
  * as many; no columns; K of 0), as may one that then nothing is read of.
@@ -397,8 +400,8 @@ t3_status t3_quant_rows(int32_t rows, int32_t cols, int32_t x_type, const void *
  *   A        int8 [M][lda], B int8 [N][ldb]: K-contiguous (T3_A_MK, T3_B_NK; T3_ERR_UNSUPPORTED otherwise)
  *   scale_a  fp32 [M], scale_b fp32 [N], device, 4-byte aligned
  * p is as for the bf16 calls with lda, ldb and K in elements of a byte: multiples of 16 (T3_ERR_ALIGN), K at most 131056, so that no
- * sum leaves 32 bits, A and B below 2^32 bytes each (T3_ERR_UNSUPPORTED).  Neither two writers nor split-K, and a tile range is of whole
- * ring steps (T3_ERR_UNSUPPORTED).
+ * sum leaves 32 bits, A and B below 2^32 bytes each (T3_ERR_UNSUPPORTED).  A tile range is of whole ring steps, and the fused call has neither
+ * two writers nor split-K (T3_ERR_UNSUPPORTED; the plain one ignores flags and split_k as t3_gemm does).
  */
 t3_status t3_gemm_i8(const t3_problem *p, const int8_t *A, const float *scale_a, const int8_t *B, const float *scale_b,
                      float *C, void *stream);
@@ -431,7 +434,7 @@ typedef struct {
  *   A        bf16 [rows][lda], B bf16 at B + e stride_b, by b_layout; lda, ldb, stride_b and K multiples of 8
  *   C        fp32 [rows][ldc], N and ldc multiples of 4; out: the groups' rows
  * The same problem and offsets give the same bits, under graph capture as well.  A call is one launch, or two (a last round of tiles that
- * would leave most of the device idle is done in smaller ones); `offsets` may change between calls and replays, not during one.
+ * would leave most of the device idle is done in smaller ones), or one for every 2^23 tiles where these are small; `offsets` may change between calls and replays, not during one.
  * T3_B_KN is the gradient to the rows of a layer whose weights are stored N x K (K and N trade places): N a multiple of 8.  A and a group's B below 2^31 elements each, C below 2^32 bytes.
  */
 t3_status t3_gemm_grouped(const t3_grouped *g, const int32_t *offsets, const void *A, const void *B, float *C,
