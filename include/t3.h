@@ -453,7 +453,7 @@ t3_status t3_gemm_grouped_i8(const t3_grouped *g, const int32_t *offsets, const 
  *   dB  fp32 at dB + e stride_b, leading dimension ldb, both multiples of 4, groups not overlapping; out, or with
  *       T3_GROUPED_ACCUMULATE added to
  * A and dC below 2^31 elements each, a group's dB below 2^32 bytes.  With ldb above 2^21, or (rows + 256) lda or (rows + 256) ldc
- * above 2^30, all of dB in less than 2^24 tiles of 64 x 64 (T3_ERR_UNSUPPORTED beyond).
+ * above 2^30, all of dB in less than 2^24 tiles of 64 x 64 (T3_ERR_UNSUPPORTED beyond).  Launches as in t3_gemm_grouped.
  */
 t3_status t3_gemm_grouped_wgrad(const t3_grouped *g, const int32_t *offsets, const void *A, const void *dC, float *dB,
                                 void *stream);

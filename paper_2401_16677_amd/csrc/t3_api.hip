@@ -547,9 +547,12 @@ t3_status check_grouped(const t3_grouped *g, bool wgrad, int size) {
 }
 
 // What the launches of products by group have in common: how grid positions fall to the workgroups, and whether results leave the caches.
-// bytes: of operands and result.  Results stream where all of it is more than the memory-side cache holds.  In us, kept and streamed,
-// and with a reader of C right behind: 8192 rows of 16 groups x 5120 x 1280, 398 MB, 136 and 105, with the reader 180 and 177; the gradient
-// of its weights, 524 MB, 181 and 137; 16384 of 8 x 8192 x 1024, 705 MB, 298 and 264, 439 and 450; 4096 of 8 x 5120 x 1280, 200 MB, 61 and 59, 79 and 82.
+// bytes: of operands and result.  Results stream where all of it is more than the memory-side cache holds.  In us, kept and streamed, and with a reader
+// of the result right behind (to bfloat16), which is what counts; operands in memory: 4096 rows of 8 groups x 5120 x 1280, 199 MB, 87 and 85, with the reader
+// 106 and 108; 8192 of 16 x 5120 x 1280, 398 MB, 157 and 151, 196 and 193; 16384 of 8 x 8192 x 1024, 705 MB, 317 and 321, 463 and 451; 16384 of 16 x 6144 x 2048,
+// 872 MB, 408 and 400, 505 and 490; gradients of weights: 4096 of 8 x 2560 x 1280, 136 MB, 59 and 45, 82 and 82; 8190 of 16 x 5120 x 1280, 524 MB, 171 and
+// 163, 287 and 268; 16384 of 32 x 4096 x 2048, 1275 MB, 409 and 381, 697 and 651.  On one set of operands again and again 2 to 3 us more than kept, with the
+// reader, up to 199 MB, and 1 to 6 % less from 398 MB on.
 void plan_rounds(t3k::Plan &q, const t3k::Choice &c, const DeviceFacts &dev, int64_t most_tiles, int64_t bytes) {
   q.tile_m = c.tile.m;
   q.tile_n = c.tile.n;

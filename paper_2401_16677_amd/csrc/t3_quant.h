@@ -1,8 +1,8 @@
 // Rows to 8-bit integers: q = the integer nearest to 127 x / a, a the row's largest magnitude, and the row's scale a / 127.
 //
 // Bound by memory: a row is read once, held in registers while its largest magnitude is found, and written once (rows that
-// do not fit are read again).  A wavefront has a row, a workgroup a long one.  bfloat16 from memory: 4096 x 6144 16 us, 4.7 TB/s, the rate of a copy; 37 x 6144
-// 4 us and 1 x 1536 2.4 us, a launch and two round trips.
+// do not fit are read again).  A wavefront has a row, a workgroup a long one.  From memory: bfloat16 4096 x 6144 16 to 18 us, 4.2 to 4.7 TB/s, the rate of a copy, float32
+// 25 us, 5.0; 4096 x 12288 31 and 48 us, 4.9 and 5.3; bfloat16 37 x 6144 4 us and 1 x 1536 2.4 us, a launch and two round trips.
 #pragma once
 
 #include "t3_device.h"

@@ -29,9 +29,9 @@
 //
 // The same kernel multiplies operands in 8 bits (I8: as many bytes a slab, 16 x 16 x 64 a product; the integer sums become floats times
 // their scales on the way out) and rows sorted by group (MODE kModeGrouped, kModeWgrad, kModeWgradAdd: see t3_groups.h; a piece of work is a tile of one group).
-// In 8 bits 4096 x 12288 x 6144 takes 240 us, 2600 TOP/s, bound by power (a library's int8 product of 8192^3: 2441).  By group, operands in memory,
-// a slab of 256 x 256 takes 1.6 us where it takes 1.22 from the caches: 8192 rows of 16 groups x 5120 x 1280 140 to 154 us, 3.4 TB/s; the gradient of their weights, which
-// is mostly the writing of 419 MB, 160 us, 4 TB/s.
+// In 8 bits 4096 x 12288 x 6144 takes 240 to 253 us, 2440 to 2600 TOP/s, bound by power (a library's int8 product of 8192^3: 2441).  By group, operands in memory,
+// a slab of 256 x 256 takes 1.6 us where it takes 1.22 from the caches: 8192 rows of 16 groups x 5120 x 1280 150 to 161 us, 2.5 TB/s; the gradient of their weights, which
+// is mostly the writing of 419 MB, 160 us, 3.3 TB/s.
 //
 // Included by the launch units only.
 #pragma once
@@ -359,7 +359,7 @@ void wide_tile_kernel(const Plan) {
 #pragma unroll
       for (int q = 0; q < NB; ++q) offB[q] = mark(offB[q], k_chunk(q) * 8 >= ktail);
       markedA = markedB = true;
-    } else if constexpr (grouped) {              // (k-rows of B past the last are past its buffer)
+    } else if constexpr (grouped) {              // (k-rows of B past the last are past its buffer: see grouped_wide_fits)
       walkA.at = walkA.end;
       walkB.at = walkB.end;
 #pragma unroll
